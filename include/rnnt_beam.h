@@ -325,7 +325,126 @@ float rnnt_beam_last_decode_ms(rnnt_beam_t *h);
 int rnnt_beam_set_profiling(rnnt_beam_t *h, int32_t on);
 int rnnt_beam_kernel_times(rnnt_beam_t *h, const char **names, float *ms, int32_t *calls, int32_t n_cap);
 
-const char *rnnt_beam_last_error(const rnnt_beam_t *h); /* NULL handle: error of the last failed create */
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators for networks that the caller runs itself: an attention decoder searched with a beam, a neural language model that rescores the
+ * n-best lists of a decode.  The caller computes the products; these calls keep its keys and values, attend over them, select the tokens
+ * and move the states of hypotheses.  All pointers are device memory unless stated; work is enqueued on hip_stream and the calls return at
+ * once; nothing is allocated, no call waits, all may be captured into a HIP graph.  Structures are plain data, versioned by struct_size;
+ * strides count elements (of rnnt_states_t: bytes).  RNNT_E_ARG with a message (rnnt_beam_last_error(NULL), of this thread) for what the host
+ * can see to be wrong; what only the device sees (tables, lengths, parents, counts) is taken as described at each call, never beyond the arrays.
+ */
+typedef enum { RNNT_TYPE_F32 = 0, RNNT_TYPE_F16 = 1, RNNT_TYPE_BF16 = 2 } rnnt_type_t;
+
+/*
+ * One step of a beam search over logits: for each of B utterances the `beam` best of the beam * V candidates
+ *   key(k, v) = scores[k] + x[k, v] - log sum_u exp x[k, u],
+ * key descending, of equal keys the smaller k V + v first.  Keys are float64, the sums of the exponentials too.  No candidates: keys of NaN or
+ * -inf, so none of an empty slot (score -inf), none of a row with a NaN or +inf.  A hypothesis with done[k] has one candidate, token eos
+ * with key scores[k]; its logits are not read.  Outputs per slot: the key, the parent slot and the token; empty slots behind the last candidate: -inf, -1,
+ * -3 (as rnnt_beam_dump_tree has them); out_done = token == eos.  scores and out_scores may be one array, done and out_done too.
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t type;              /* of the logits, rnnt_type_t */
+  int32_t B, beam, V;        /* beam <= 16, beam * V < 2^31 */
+  int32_t eos;               /* -1: none; done and out_done are NULL then */
+  const void *logits;        /* [B, beam, V], the last dimension contiguous, rows at any address of their type */
+  int64_t stride_b, stride_k;
+  const double *scores;      /* [B, beam] */
+  const uint8_t *done;       /* [B, beam] 0 / 1, or NULL */
+  double *out_scores;        /* [B, beam] */
+  int32_t *out_parent, *out_token;
+  uint8_t *out_done;         /* NULL unless eos >= 0 */
+  void *workspace;           /* of rnnt_select_tokens_workspace bytes, 16-byte aligned; its contents mean nothing between calls, calls
+                                that may overlap in time need one each.  NULL where that is 0 */
+  int64_t workspace_bytes;
+} rnnt_select_t;
+int64_t rnnt_select_tokens_workspace(int32_t B, int32_t beam, int32_t V);
+int rnnt_select_tokens(const rnnt_select_t *args, void *hip_stream);
+
+/*
+ * The states of hypotheses moved to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]] for every tensor, as if all
+ * were read before any is written.  Parents outside 0 .. beam - 1 (an empty slot's -1) leave the slot as it is.  Up to 16 tensors
+ * [lead, B, beam, inner, row_bytes]; rows that overlap are refused, tensors of one call must not overlap each other.
+ */
+typedef struct {
+  void *data;
+  int64_t lead_stride, b_stride, slot_stride, inner_stride; /* bytes, not negative */
+  int64_t row_bytes;                                        /* contiguous */
+  int32_t lead, inner;
+} rnnt_states_t;
+int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rnnt_states_t *states /* host */, int32_t n, void *hip_stream);
+
+/*
+ * A paged cache of one attention layer's keys and values, in the caller's arrays.  A row, the `dim` values of one token and key head, is kept
+ * as y 2^s: s the smallest exponent with max |x| <= 448 2^s (RNNT_CACHE_E4M3, y in OCP e4m3) or max |x| < 2^15 2^s (RNNT_CACHE_F16, y in
+ * float16), at least -126; y = x 2^-s rounded to the nearest, ties to even.  A row with a NaN or an infinity is kept as y = 0, exponent byte 255 and reads
+ * as NaN.  Position p of sequence b lies in page table[b, p / page_size], place p % page_size.  Positions that are negative or
+ * beyond the table, and those whose page is outside 0 .. n_pages - 1, are not there: not written, read as zeros, not attended.
+ */
+typedef enum { RNNT_CACHE_E4M3 = 0, RNNT_CACHE_F16 = 1 } rnnt_cache_format_t;
+typedef struct {
+  uint32_t struct_size;
+  int32_t format;              /* rnnt_cache_format_t */
+  int32_t n_pages, page_size;  /* page_size a power of two up to 4096; n_pages * heads * page_size < 2^32 - 1,
+                                  width * page_size at most 2^30 */
+  int32_t heads, dim;          /* key heads; dim a multiple of 16, 16 .. 256 */
+  void *k, *v;                 /* [n_pages, heads, page_size, dim], 16-byte aligned */
+  uint8_t *k_exp, *v_exp;      /* [n_pages, heads, page_size]: s + 127 */
+  const int32_t *table;        /* [B, width], rows table_stride apart */
+  int64_t table_stride;
+  int32_t width;
+} rnnt_cache_t;
+typedef struct { /* rows of a network: [B, n, heads, dim], dim contiguous */
+  void *data;
+  int64_t stride_b, stride_n, stride_h;
+} rnnt_rows_t;
+
+/* Rows (b, i), i < count[b] (NULL: all n) to positions start[b] + i, and back.  Two rows written to one position: one of them.  Read rows
+ * from count[b] on are zeros. */
+int rnnt_cache_write(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t *v, int32_t type, int32_t B, int32_t n,
+                     const int32_t *start, const int32_t *count, void *hip_stream);
+int rnnt_cache_read(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t *v, int32_t type, int32_t B, int32_t n,
+                    const int32_t *start, const int32_t *count, void *hip_stream);
+
+/*
+ * Attention of new tokens over the cache, soft-max of scale q.k: sequence b holds lens[b] tokens (negative: none) at positions 0 .., all of which every query
+ * sees, and behind them the rows of `tree` new nodes at positions lens[b] + i, written before this call.  Node i's parent is
+ * parents[b, i], a node before it or -1; a query sees its node and the node's ancestors.  parents NULL: a chain, node i's parent is i - 1
+ * (one token, or a chunk).  Queries are the last n nodes (n = tree: all; fewer where rows of earlier nodes are in the cache but not asked for).
+ * A node whose parent is neither -1 nor a node before it is padding: its output, and that of nodes below it, is zero, its rows need not
+ * have been written.  A query that sees nothing gets zeros; one that sees a row of NaN, or is not finite itself, NaN.  Rows that a query does not see
+ * have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; the value rows of a
+ * sequence's head, those of zeros aside, are taken as within 2^100 of the first 64 of them.  Outputs repeat bit for bit.
+ */
+typedef struct {
+  uint32_t struct_size;
+  int32_t type;                /* of q and out, rnnt_type_t */
+  int32_t B, n, tree;          /* n <= tree; with parents tree <= 1024 */
+  int32_t q_heads;             /* a multiple of the cache's heads */
+  float scale;
+  int32_t max_len;             /* host's bound of lens + tree, by which the work is split: a smaller one than the lengths only costs time */
+  rnnt_rows_t q;               /* [B, n, q_heads, dim] */
+  void *out;                   /* [B, n, q_heads, dim], contiguous */
+  const int32_t *lens;         /* [B] */
+  const int32_t *parents;      /* [B, tree] or NULL */
+  void *workspace;             /* of rnnt_cache_attend_workspace bytes, 16-byte aligned; as that of rnnt_select_t */
+  int64_t workspace_bytes;
+} rnnt_attend_t;
+int64_t rnnt_cache_attend_workspace(const rnnt_cache_t *cache, const rnnt_attend_t *args);
+int rnnt_cache_attend(const rnnt_cache_t *cache, const rnnt_attend_t *args, void *hip_stream);
+
+/*
+ * The prefix tree of n-best lists (host arrays, no GPU): tokens [B, beam, cap] and lens [B, beam] as rnnt_beam_results gives them.  Every distinct prefix
+ * of an utterance is a node: its last token in node_token [B, max_nodes], its parent in node_parent [B, max_nodes], a node before it, -1 for
+ * a first token, -2 behind the last of n_nodes[b] nodes (padding of rnnt_cache_attend).  leaf [B, beam]: the node at which a hypothesis ends, -1
+ * for an empty one.  Returns the largest n_nodes; RNNT_E_ARG where max_nodes is too small.
+ */
+int rnnt_nbest_tree(const int32_t *tokens, const int32_t *lens, int32_t B, int32_t beam, int32_t cap, int32_t max_nodes, int32_t *node_token,
+                    int32_t *node_parent, int32_t *leaf, int32_t *n_nodes);
+
+/* NULL handle: error of the last failed create, or of the last failed call above, on this thread */
+const char *rnnt_beam_last_error(const rnnt_beam_t *h);
 void rnnt_beam_destroy(rnnt_beam_t *h);
 void rnnt_lm_destroy(rnnt_lm_t *lm);
 

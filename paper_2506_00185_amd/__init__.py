@@ -6,3 +6,4 @@ arguments and uses PyTorch only to hold device memory and streams.  There is no
 CPU fallback: without the built library every call raises.
 """
 from .binding import (ALSD, AES, BeamDecoder, NGramLM, RnntBeamError, library_path, load_library)  # noqa: F401
+from .tokens import KVCache, nbest_tree, reorder_states, select_tokens  # noqa: F401

@@ -19,7 +19,9 @@ EXPORTS = ["rnnt_beam_create", "rnnt_lm_create", "rnnt_beam_decode", "rnnt_beam_
            "rnnt_beam_last_decode_ms", "rnnt_beam_set_profiling", "rnnt_beam_kernel_times", "rnnt_beam_last_error",
            "rnnt_beam_destroy", "rnnt_lm_destroy", "rnnt_beam_debug_block_map", "rnnt_beam_decode_static", "rnnt_beam_debug_set_spin_limit",
            "rnnt_beam_last_step_loop", "rnnt_beam_debug_stall_resident", "rnnt_beam_debug_rebuild_resident",
-           "rnnt_beam_debug_resident_groups", "rnnt_beam_debug_gates"]
+           "rnnt_beam_debug_resident_groups", "rnnt_beam_debug_gates", "rnnt_select_tokens", "rnnt_select_tokens_workspace",
+           "rnnt_reorder_states", "rnnt_cache_write", "rnnt_cache_read", "rnnt_cache_attend", "rnnt_cache_attend_workspace",
+           "rnnt_nbest_tree"]
 
 
 class RnntBeamError(RuntimeError):
@@ -91,6 +93,8 @@ def load_library():
         lib.rnnt_beam_last_decode_ms.argtypes = [C.c_void_p]
         lib.rnnt_beam_destroy.argtypes = [C.c_void_p]
         lib.rnnt_lm_destroy.argtypes = [C.c_void_p]
+        lib.rnnt_select_tokens_workspace.restype = C.c_int64
+        lib.rnnt_cache_attend_workspace.restype = C.c_int64
         _lib = lib
     return _lib
 

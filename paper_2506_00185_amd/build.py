@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librnnt_beam.so")
 # (source, defines): compiled at the same time, then linked
-UNITS = [("rnnt_beam.hip", []), ("rnnt_lm.hip", []), ("rnnt_resident.hip", [])] + [
+UNITS = [("rnnt_beam.hip", []), ("rnnt_lm.hip", []), ("rnnt_resident.hip", []), ("rnnt_tokens.hip", []), ("rnnt_cache.hip", [])] + [
+    ("attend_kernels.hip", [f"-DRB_AT_TYPE={t}", f"-DRB_AT_FMT={f}"]) for t in ("TypeF32", "TypeF16", "TypeBf16") for f in (8, 16)] + [
     ("resident_kernels.hip", [f"-DRB_RES_FULL={full}", f"-DRB_RES_FORM={form}", f"-DRB_RES_ST={st}"])
     for st in (0, 1) for full in (1, 0) for form in (0, 1, 2)]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

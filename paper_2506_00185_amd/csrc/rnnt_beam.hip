@@ -24,6 +24,7 @@
 #include "kernels_persistent.h"
 #include "lm.h"
 #include "resident.h"
+#include "token_host.h"
 
 using namespace rb;
 
@@ -37,7 +38,7 @@ static std::mutex g_scratch_mutex;
 
 namespace {
 
-thread_local std::string g_create_error;
+thread_local std::string g_create_error;  // and of calls without a handle
 
 inline float host_bf16_round(float x) {
   uint32_t u;
@@ -1734,3 +1735,5 @@ void rnnt_beam_destroy(rnnt_beam_t *h) {
 }
 
 }  // extern "C"
+
+void rb::set_call_error(const char *msg) { g_create_error = msg; }

@@ -1,0 +1,445 @@
+// Selection of a beam's best tokens from logits that the caller computed, and the reordering of states by the parents it
+// names (rnnt_select_tokens, rnnt_reorder_states).
+#pragma once
+#include "token_types.h"
+
+namespace rb {
+
+// ---- soft-max statistics in float64
+// The keys of an utterance's hypotheses are compared with each other, and the sums of rows decide between candidates whose logits differ by
+// little: float32 exponentials leave 1e-8 to 1e-7 of a row's log sum open.  float64 multiply-adds run at the rate of float32 ones here, so
+// the exponential is a polynomial in float64: 2^t = 2^n 2^f, n = t rounded, and for 2^f the polynomial of degree 7 through the
+// Chebyshev points of [-1/2, 1/2], off by at most 5.5e-11 of its value.  (Sums that are brought to a common reference are multiplied by
+// the library's exp, or that error would count again.)
+__device__ __forceinline__ double exp2_d(double t) {
+  t = fmax(t, -3000.);  // of -inf too: 0
+  const double n = __builtin_rint(t), f = t - n;
+  double p = 1.5303699794189107e-05;
+  p = fma(p, f, 0.0001546972916352668);
+  p = fma(p, f, 0.0013333478479379338);
+  p = fma(p, f, 0.009618025613514537);
+  p = fma(p, f, 0.05550410906315832);
+  p = fma(p, f, 0.2402265121349604);
+  p = fma(p, f, 0.693147180556837);
+  p = fma(p, f, 0.9999999999595622);
+  return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
+constexpr int kSelTile = 32;   // logits a lane holds at a time
+constexpr int kSelBuf = 64;    // candidates that a wave ranks at a time: one per lane
+constexpr int kSelLists = 64;  // lists that a wave joins: one per lane
+
+// What a wave knows of its part of a row: the `beam` largest logits, in lanes 0 .. beam - 1 in order (of equal ones the smaller index
+// first; -inf behind the last), and sum exp(x - ref), each lane's share of it.
+struct RowPart {
+  float v = -INFINITY;
+  int i = 0x7fffffff;
+  double sum = 0.;
+  float ref = -INFINITY;
+  bool bad = false;  // a NaN or +inf among them (of this lane)
+};
+
+struct CandBuf {
+  float v[kSelBuf];
+  int i[kSelBuf];
+};
+
+// Lanes 0 .. n - 1 hold candidates: each one's rank among them goes to the list of the best `beam`.
+__device__ __forceinline__ void rank_candidates(float v, int i, int n, int beam, CandBuf &buf, float &out_v, int &out_i) {
+  const int lane = threadIdx.x & 63;
+  int rank = 0;
+  for (int j = 0; j < n; ++j) rank += comes_before_count(readlane_f(v, j), __builtin_amdgcn_readlane(i, j), v, i);
+  wave_lds_order();
+  if (lane < beam) {  // (places without a candidate come as equal ones, of which but one rank is filled)
+    buf.v[lane] = -INFINITY;
+    buf.i[lane] = 0x7fffffff;
+  }
+  wave_lds_order();
+  if (lane < n && rank < beam) {
+    buf.v[rank] = v;
+    buf.i[rank] = i;
+  }
+  wave_lds_order();
+  out_v = lane < beam ? buf.v[lane] : -INFINITY;
+  out_i = lane < beam ? buf.i[lane] : 0x7fffffff;
+  wave_lds_order();
+}
+
+// One tile of 64 * E logits of a row from index `base` on, lane l's in x: adds them to the sum and the list.
+// The list: a bound that the `beam` best reach is the beam-th largest of the lanes' maxima, or what the list holds already; those logits that
+// reach it, few more than `beam` as a rule, are collected and ranked.  Where more than a wave ranks at a time reach it (many equal
+// logits), the best are taken out one after the other instead.
+template <int E, int VE>
+__device__ __forceinline__ void take_tile(const float (&x)[E], int base, int beam, RowPart &part, CandBuf &buf) {
+  const int lane = threadIdx.x & 63;
+  auto index = [&](int e) { return base + (e / VE) * 64 * VE + lane * VE + e % VE; };
+  float top = x[0];
+  bool bad = false;
+#pragma unroll
+  for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
+#pragma unroll
+  for (int e = 0; e + 1 < E; e += 2) bad |= __builtin_isunordered(x[e], x[e + 1]);
+  if constexpr (E % 2) bad |= __builtin_isunordered(x[E - 1], x[E - 1]);
+  part.bad |= bad || top == INFINITY;
+  const float most = wave_max(top);
+  if (!(most > -INFINITY)) return;
+  if (!(most < part.ref + 500.f)) {  // (the first tile too; float64 holds exp(500) times exp(200) more)
+    const float ref = most < INFINITY ? most : 0.f;
+    part.sum *= part.ref == -INFINITY ? 0. : exp((double)part.ref - ref);
+    part.ref = ref;
+  }
+  const double ref = part.ref;
+#pragma unroll
+  for (int e = 0; e < E; ++e) part.sum += exp2_d(((double)x[e] - ref) * kLog2E);
+
+  const float last = readlane_f(part.v, beam - 1);
+  if (!(most > last)) return;  // equal ones come after those of the list, whose indices are smaller
+  float bound = from_orderable(orderable(last) + 1);
+  if (__popcll(__ballot(top > last)) >= beam) {
+    float rest = top, m = most;
+    int n = 0;
+    while (true) {
+      const uint64_t at = __ballot(rest == m);
+      n += __popcll(at);
+      if (n >= beam) break;
+      rest = rest == m ? -INFINITY : rest;
+      m = wave_max(rest);
+    }
+    bound = m;
+  }
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const bool in = x[e] >= bound;
+    const uint64_t at = __ballot(in);
+    if (at) {
+      const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
+      if (in && pos < kSelBuf) {
+        buf.v[pos] = x[e];
+        buf.i[pos] = index(e);
+      }
+      n += __popcll(at);
+    }
+  }
+  const int held = __popcll(__ballot(lane < beam && part.v > -INFINITY));
+  if (n + held > kSelBuf) {
+    uint32_t taken = 0;
+    n = 0;
+    while (n < beam) {
+      float v = -INFINITY;
+      int i = 0x7fffffff, at = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const bool better = !(taken >> e & 1) && x[e] > v;
+        v = better ? x[e] : v;
+        i = better ? index(e) : i;
+        at = better ? e : at;
+      }
+      const int own = i;
+      wave_best(v, i);
+      if (!(v > last)) break;
+      if (own == i) taken |= 1u << at;
+      wave_lds_order();
+      if (lane == 0) {
+        buf.v[n] = v;
+        buf.i[n] = i;
+      }
+      ++n;
+    }
+  }
+  wave_lds_order();
+  if (lane < held) {
+    buf.v[n + lane] = part.v;
+    buf.i[n + lane] = part.i;
+  }
+  n += held;
+  wave_lds_order();
+  rank_candidates(lane < n ? buf.v[lane] : -INFINITY, lane < n ? buf.i[lane] : 0x7fffffff, n, beam, buf, part.v, part.i);
+}
+
+// A wave's part [begin, end) of a row.
+template <typename T, int E>
+__device__ __forceinline__ void scan_row(const T *row, int begin, int end, int beam, RowPart &part, CandBuf &buf) {
+  constexpr int VE = 16 / sizeof(T), NV = E / VE;
+  const int lane = threadIdx.x & 63;
+  for (int base = begin; base < end; base += 64 * E) {
+    float x[E];
+    if (base + 64 * E <= end) {
+      T raw[NV][VE];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load16(row + base + i * 64 * VE + lane * VE, raw[i]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) x[i * VE + j] = to_float(raw[i][j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int at = base + i * 64 * VE + lane * VE;
+        if (at + VE <= end) {
+          T raw[VE];
+          load16(row + at, raw);
+#pragma unroll
+          for (int j = 0; j < VE; ++j) x[i * VE + j] = to_float(raw[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VE; ++j) x[i * VE + j] = at + j < end ? to_float(row[at + j]) : -INFINITY;
+        }
+      }
+    }
+    take_tile<E, VE>(x, base, beam, part, buf);
+  }
+}
+
+__device__ __forceinline__ double wave_sum_d(double v) {
+  v += dpp_d<kDppXor1>(v);
+  v += dpp_d<kDppXor2>(v);
+  v += dpp_d<kDppHalfMirror>(v);
+  v += dpp_d<kDppMirror>(v);
+  return (readlane_d(v, 0) + readlane_d(v, 16)) + (readlane_d(v, 32) + readlane_d(v, 48));
+}
+
+// A list as it is handed on: the best of a part of a row and the sum of its exponentials.
+struct SelList {
+  float v[kMaxBeam];
+  int i[kMaxBeam];
+};
+struct SelStat {
+  double sum;  // NaN: a NaN or +inf among the logits
+  float ref;   // -inf: all logits were
+  int pad;
+};
+
+struct SelectArgs {
+  const void *logits;
+  int64_t stride_b, stride_k;
+  const double *scores;
+  const uint8_t *done;
+  double *out_scores;
+  int *out_parent, *out_token;
+  uint8_t *out_done;
+  SelList *lists;  // [B][beam][parts]
+  SelStat *stats;
+  int B, beam, V, eos, parts, part_len;
+};
+
+struct SelJoin {
+  SelList list[kSelLists];
+  SelStat stat[kSelLists];
+  double lse[kMaxBeam], score[kMaxBeam], cand_key[kSelLists * kMaxBeam];
+  int cand_at[kSelLists * kMaxBeam];
+  int n;
+};
+
+// One wave: the `beam` best of an utterance from the lists of its rows (sh.list[k * parts + p]).  A bound that they reach is the beam-th largest of
+// the lists' first candidates; each lane hands on those of its list that reach it, and they are ranked by (key descending, flat index
+// ascending).
+__device__ __forceinline__ void join_lists(const SelectArgs &a, int b, SelJoin &sh) {
+  const int lane = threadIdx.x & 63, beam = a.beam, parts = a.parts, n_lists = beam * parts;
+  const int k = lane / parts;
+  const bool have = lane < n_lists;
+  if (lane == 0) sh.n = 0;
+  // log sum exp of every row
+  SelStat st = have ? sh.stat[lane] : SelStat{0., -INFINITY, 0};
+  float ref = -INFINITY;
+  if (have)
+    for (int p = 0; p < parts; ++p) ref = fmaxf(ref, sh.stat[k * parts + p].ref);
+  // (a part that held nothing but -inf, or NaN: its sum is 0, or NaN, whatever it is multiplied by)
+  st.sum *= st.ref > -INFINITY ? exp((double)st.ref - ref) : 1.;
+  wave_lds_order();
+  if (have) sh.stat[lane].sum = st.sum;
+  wave_lds_order();
+  bool finished = false;
+  if (lane < beam) {
+    double s = 0.;
+    for (int p = 0; p < parts; ++p) s += sh.stat[lane * parts + p].sum;
+    float r = -INFINITY;
+    for (int p = 0; p < parts; ++p) r = fmaxf(r, sh.stat[lane * parts + p].ref);
+    sh.score[lane] = a.scores[(int64_t)b * beam + lane];
+    finished = a.done && a.done[(int64_t)b * beam + lane];
+    sh.lse[lane] = finished ? 0. : (double)r + log(s);
+    if (finished)  // its one candidate: eos, with the score that it has
+      for (int p = 0; p < parts; ++p) {
+        sh.list[lane * parts + p].v[0] = p == 0 ? 0.f : -INFINITY;
+        sh.list[lane * parts + p].i[0] = a.eos;
+        sh.list[lane * parts + p].v[1] = -INFINITY;
+      }
+  }
+  wave_lds_order();
+  const double score = have ? sh.score[k] : 0., lse = have ? sh.lse[k] : 0.;
+  auto key_of = [&](float v) {
+    const double key = score + ((double)v - lse);
+    return key == key && v > -INFINITY ? key : (double)-INFINITY;
+  };
+  const double head = have ? key_of(sh.list[lane].v[0]) : -INFINITY;
+  int rank = 0;
+  for (int j = 0; j < n_lists; ++j) rank += comes_before_count(readlane_d(head, j), j, head, lane);
+  const uint64_t at = __ballot(have && rank == beam - 1);
+  const double bound = readlane_d(head, __ffsll((unsigned long long)at) - 1);
+  int mine = 0;
+  if (have && head > -INFINITY)
+    while (mine < beam) {
+      const double key = key_of(sh.list[lane].v[mine]);
+      if (!(key >= bound && key > -INFINITY)) break;
+      ++mine;
+    }
+  if (mine) {
+    const int pos = atomicAdd(&sh.n, mine);
+    for (int j = 0; j < mine; ++j) {
+      sh.cand_key[pos + j] = key_of(sh.list[lane].v[j]);
+      sh.cand_at[pos + j] = k * a.V + sh.list[lane].i[j];
+    }
+  }
+  wave_lds_order();
+  const int n = sh.n;
+  const int64_t out = (int64_t)b * beam;
+  for (int c = lane; c < n; c += 64) {
+    const double key = sh.cand_key[c];
+    const int flat = sh.cand_at[c];
+    int r = 0;
+    for (int j = 0; j < n; ++j) r += comes_before_count(sh.cand_key[j], sh.cand_at[j], key, flat);
+    if (r < beam) {
+      const int parent = flat / a.V, token = flat - parent * a.V;
+      a.out_scores[out + r] = key;
+      a.out_parent[out + r] = parent;
+      a.out_token[out + r] = token;
+      if (a.out_done) a.out_done[out + r] = token == a.eos;
+    }
+  }
+  for (int r = n + lane; r < beam; r += 64) {  // empty slots
+    a.out_scores[out + r] = -INFINITY;
+    a.out_parent[out + r] = -1;
+    a.out_token[out + r] = -3;
+    if (a.out_done) a.out_done[out + r] = 0;
+  }
+}
+
+__device__ __forceinline__ void put_list(const RowPart &part, double sum, bool bad, int beam, SelList &list, SelStat &stat) {
+  const int lane = threadIdx.x & 63;
+  if (lane < beam) {
+    list.v[lane] = part.v;
+    list.i[lane] = part.i;
+  }
+  if (lane == 0) stat = SelStat{bad ? (double)NAN : sum, part.ref, 0};
+}
+
+// ---- everything of an utterance in one block of 16 waves, parts = 16 / beam of them for a row: no workspace, one launch
+template <typename TT>
+__global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
+  typedef typename TT::T T;
+  __shared__ SelJoin sh;
+  __shared__ CandBuf buf[16];
+  const int b = blockIdx.x, wave = threadIdx.x >> 6, k = wave / a.parts, p = wave - k * a.parts;
+  if (k < a.beam) {
+    RowPart part;
+    if (!(a.done && a.done[(int64_t)b * a.beam + k])) {
+      const T *row = static_cast<const T *>(a.logits) + b * a.stride_b + k * a.stride_k;
+      const int begin = min(p * a.part_len, a.V);
+      scan_row<T, 16>(row, begin, min(begin + a.part_len, a.V), a.beam, part, buf[wave]);
+    }
+    const double sum = wave_sum_d(part.sum);
+    put_list(part, sum, __any(part.bad), a.beam, sh.list[wave], sh.stat[wave]);
+  }
+  __syncthreads();
+  if (wave == 0) join_lists(a, b, sh);
+}
+
+// ---- many blocks for a row: each leaves the best of its part, a second launch joins them
+template <typename TT>
+__global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
+  typedef typename TT::T T;
+  __shared__ CandBuf buf[4];
+  __shared__ SelList list[4];
+  __shared__ SelStat stat[4];
+  const int p = blockIdx.x % a.parts, row_i = blockIdx.x / a.parts, b = row_i / a.beam, k = row_i - b * a.beam;
+  if (a.done && a.done[row_i]) return;  // (the join takes nothing from its lists)
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const T *row = static_cast<const T *>(a.logits) + b * a.stride_b + k * a.stride_k;
+  const int len = a.part_len >> 2, begin = min(p * a.part_len + wave * len, a.V);
+  RowPart part;
+  scan_row<T, kSelTile>(row, begin, min(begin + len, a.V), a.beam, part, buf[wave]);
+  const double sum = wave_sum_d(part.sum);
+  put_list(part, sum, __any(part.bad), a.beam, list[wave], stat[wave]);
+  __syncthreads();
+  if (wave) return;
+  const int n = 4 * a.beam, w = lane / a.beam, e = lane - w * a.beam;  // at most 64
+  float v;
+  int i;
+  rank_candidates(lane < n ? list[w].v[e] : -INFINITY, lane < n ? list[w].i[e] : 0x7fffffff, n, a.beam, buf[0], v, i);
+  const int64_t at = (int64_t)row_i * a.parts + p;
+  if (lane < a.beam) {
+    a.lists[at].v[lane] = v;
+    a.lists[at].i[lane] = i;
+  }
+  if (lane == 0) {
+    float ref = -INFINITY;
+    double s = 0.;
+    for (int j = 0; j < 4; ++j) ref = fmaxf(ref, stat[j].ref);
+    for (int j = 0; j < 4; ++j) s += stat[j].sum * (stat[j].ref > -INFINITY ? exp((double)stat[j].ref - ref) : 1.);
+    a.stats[at] = SelStat{s, ref, 0};
+  }
+}
+
+static __global__ __launch_bounds__(256) void k_select_join(SelectArgs a) {
+  __shared__ SelJoin sh;
+  const int b = blockIdx.x, n = a.beam * a.parts;
+  const int64_t first = (int64_t)b * n;
+  for (int e = threadIdx.x; e < n * kMaxBeam; e += 256) {
+    const int l = e / kMaxBeam, j = e % kMaxBeam;
+    const bool there = j < a.beam && !(a.done && a.done[(int64_t)b * a.beam + l / a.parts]);
+    sh.list[l].v[j] = there ? a.lists[first + l].v[j] : -INFINITY;
+    sh.list[l].i[j] = there ? a.lists[first + l].i[j] : 0x7fffffff;
+    if (j == 0) sh.stat[l] = there ? a.stats[first + l] : SelStat{0., -INFINITY, 0};
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) join_lists(a, b, sh);
+}
+
+// ---- states of hypotheses to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]]
+// A thread reads its column of all slots that move and then writes them, so that no copy of the tensor is needed and each byte is read and
+// written once; slots that stay where they are are neither read for themselves nor written.
+struct StateView {  // strides in bytes
+  char *data;
+  int64_t lead_stride, b_stride, slot_stride, inner_stride, row_bytes;
+  int lead, inner;
+  int chunks;       // blocks for one row
+  int first_block;  // of this tensor
+};
+constexpr int kMaxStates = 16;
+struct ReorderArgs {
+  const int *parent;
+  int B, beam, n;
+  StateView s[kMaxStates];
+};
+
+// V: the widest access that every address and length of the launch's tensors allows
+template <typename V, int BEAM>
+__global__ __launch_bounds__(256) void k_reorder(ReorderArgs a) {
+  int t = 0;
+  while (t + 1 < a.n && (int)blockIdx.x >= a.s[t + 1].first_block) ++t;
+  const StateView &s = a.s[t];
+  const int block = blockIdx.x - s.first_block, chunk = block % s.chunks;
+  int row = block / s.chunks;
+  const int inner = row % s.inner;
+  row /= s.inner;
+  const int b = row % a.B, lead = row / a.B;
+  int parent[BEAM];
+#pragma unroll
+  for (int k = 0; k < BEAM; ++k) {
+    const int p = k < a.beam ? a.parent[(int64_t)b * a.beam + k] : k;
+    parent[k] = p >= 0 && p < a.beam ? p : k;  // an empty slot keeps what it holds
+  }
+  const int64_t at = ((int64_t)chunk * 256 + threadIdx.x) * sizeof(V);
+  if (at >= s.row_bytes) return;
+  char *p = s.data + lead * s.lead_stride + b * s.b_stride + inner * s.inner_stride + at;
+  const int64_t slot_stride = s.slot_stride;
+  V v[BEAM];
+#pragma unroll
+  for (int k = 0; k < BEAM; ++k)
+    if (parent[k] != k) v[k] = *reinterpret_cast<const V *>(p + parent[k] * slot_stride);
+#pragma unroll
+  for (int k = 0; k < BEAM; ++k)
+    if (parent[k] != k) *reinterpret_cast<V *>(p + k * slot_stride) = v[k];
+}
+
+}  // namespace rb

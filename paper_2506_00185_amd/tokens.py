@@ -1,0 +1,310 @@
+"""Operators for networks that the caller runs itself: ctypes binding of rnnt_select_tokens, rnnt_reorder_states,
+rnnt_cache_write / read / attend and rnnt_nbest_tree.  Argument checks and marshalling only; include/rnnt_beam.h says what each does.
+
+Tensors live on one GPU; work goes to ``stream`` (default: the current stream of that GPU) and the calls return without
+waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph."""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+
+import numpy as np
+
+from .binding import RnntBeamError, _check, load_library
+
+_FORMATS = {"e4m3": 0, "f16": 1}
+
+
+class _Select(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("B", C.c_int32), ("beam", C.c_int32), ("V", C.c_int32),
+                ("eos", C.c_int32), ("logits", C.c_void_p), ("stride_b", C.c_int64), ("stride_k", C.c_int64),
+                ("scores", C.c_void_p), ("done", C.c_void_p), ("out_scores", C.c_void_p), ("out_parent", C.c_void_p),
+                ("out_token", C.c_void_p), ("out_done", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class _States(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("lead_stride", C.c_int64), ("b_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("inner_stride", C.c_int64), ("row_bytes", C.c_int64), ("lead", C.c_int32), ("inner", C.c_int32)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("format", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("heads", C.c_int32), ("dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p),
+                ("v_exp", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64), ("width", C.c_int32)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_n", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class _Attend(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("B", C.c_int32), ("n", C.c_int32), ("tree", C.c_int32),
+                ("q_heads", C.c_int32), ("scale", C.c_float), ("max_len", C.c_int32), ("q", _Rows), ("out", C.c_void_p),
+                ("lens", C.c_void_p), ("parents", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+def _refuse(ok, what):
+    if not ok:
+        raise RnntBeamError(what)
+
+
+def _types():
+    import torch
+    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+_TYPES = None
+
+
+def _type_of(t, what):
+    global _TYPES
+    if _TYPES is None:
+        _TYPES = _types()
+    code = _TYPES.get(t.dtype)
+    _refuse(code is not None, f"{what} must be float32, float16 or bfloat16")
+    return code
+
+
+def _array(t, what, dtype, shape, device):
+    """Pointer of a contiguous tensor of that type, shape and device."""
+    _refuse(t.dtype == dtype, f"{what} must be {dtype}")
+    _refuse(t.device == device, f"{what} is on {t.device}, not on {device}")
+    _refuse(tuple(t.shape) == shape, f"{what} must have shape {shape}, not {tuple(t.shape)}")
+    _refuse(t.is_contiguous(), f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+class _Call:
+    """Device and stream of a call: ``with _Call(tensor, stream, inputs) as raw`` gives the stream's pointer; allocations inside belong to it."""
+
+    def __init__(self, t, stream, inputs):
+        import torch
+        _refuse(t.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
+        self.stack = None
+        if torch.cuda.current_device() != t.device.index:
+            self.stack = contextlib.ExitStack()
+            self.stack.enter_context(torch.cuda.device(t.device))
+        current = torch.cuda.current_stream(t.device)
+        if stream is not None and stream != current:
+            _refuse(stream.device == t.device, f"the stream is of {stream.device}, the tensors are on {t.device}")
+            for x in inputs:  # of another stream: not to be given away before this call has used them
+                if x is not None:
+                    x.record_stream(stream)
+            self.stack = self.stack or contextlib.ExitStack()
+            self.stack.enter_context(torch.cuda.stream(stream))
+        self.raw = (stream or current).cuda_stream
+
+    def __enter__(self):
+        return C.c_void_p(self.raw)
+
+    def __exit__(self, *exc):
+        if self.stack is not None:
+            self.stack.close()
+
+
+def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
+    """rnnt_select_tokens: one step of a beam search over logits [B, beam, V] (float32, float16 or bfloat16, last dimension contiguous) with
+    the hypotheses' scores float64 [B, beam].  Returns (scores float64, parents int32, tokens int32, done bool or None), each [B, beam].
+    ``eos``: the token that finishes a hypothesis (-1: none), ``done`` bool [B, beam]: which have finished.  ``out``: such a tuple to write
+    to; it may hold ``scores`` and ``done`` themselves."""
+    import torch
+    _refuse(logits.dim() == 3, "logits must be [B, beam, V]")
+    B, beam, V = logits.shape
+    _refuse(V >= 1 and (V == 1 or logits.stride(2) == 1), "the last dimension of logits must be contiguous")
+    dev = logits.device
+    s = _Select(struct_size=C.sizeof(_Select), type=_type_of(logits, "logits"), B=B, beam=beam, V=V, eos=eos, logits=logits.data_ptr(),
+                stride_b=logits.stride(0), stride_k=logits.stride(1))
+    s.scores = _array(scores, "scores", torch.float64, (B, beam), dev)
+    if done is not None:
+        s.done = _array(done, "done", torch.bool, (B, beam), dev)
+    lib = load_library()
+    with _Call(logits, stream, (logits, scores, done) + tuple(out or ())) as raw:
+        if out is None:
+            out = (torch.empty((B, beam), dtype=torch.float64, device=dev), torch.empty((B, beam), dtype=torch.int32, device=dev),
+                   torch.empty((B, beam), dtype=torch.int32, device=dev),
+                   torch.empty((B, beam), dtype=torch.bool, device=dev) if eos >= 0 else None)
+            s.out_scores, s.out_parent, s.out_token = (t.data_ptr() for t in out[:3])
+        else:
+            _refuse(len(out) == 4, "out must be (scores, parents, tokens, done)")
+            s.out_scores = _array(out[0], "out scores", torch.float64, (B, beam), dev)
+            s.out_parent = _array(out[1], "out parents", torch.int32, (B, beam), dev)
+            s.out_token = _array(out[2], "out tokens", torch.int32, (B, beam), dev)
+            if out[3] is not None:
+                _array(out[3], "out done", torch.bool, (B, beam), dev)
+        if out[3] is not None:
+            s.out_done = out[3].data_ptr()
+        s.workspace_bytes = lib.rnnt_select_tokens_workspace(B, beam, V)
+        if s.workspace_bytes:
+            work = torch.empty(s.workspace_bytes, dtype=torch.uint8, device=dev)
+            s.workspace = work.data_ptr()
+        _check(lib.rnnt_select_tokens(C.byref(s), raw))
+    return out
+
+
+def _rows_of(shape, strides, what):
+    """(rows, stride, run) of trailing dimensions: a run of contiguous elements, repeated at one stride."""
+    run, dims = 1, list(zip(shape, strides))
+    while dims and (dims[-1][0] == 1 or dims[-1][1] == run):
+        run *= dims.pop()[0]
+    dims = [d for d in dims if d[0] != 1]
+    if not dims:
+        return 1, 0, run
+    rows, stride = dims.pop()
+    while dims and dims[-1][1] == stride * rows:
+        rows *= dims.pop()[0]
+    _refuse(not dims, f"{what}: the dimensions behind the slots must be one run of elements or runs at one stride")
+    return rows, stride, run
+
+
+def reorder_states(parents, states, lead=0, stream=None):
+    """rnnt_reorder_states: state[b, k] = state[b, parents[b, k]] in place, for each of up to 16 tensors of any type, [B, beam, ...] behind
+    ``lead`` (0 or 1) dimensions, e.g. of layers.  parents int32 [B, beam]; those outside 0 .. beam - 1 leave their slot as it is."""
+    import torch
+    _refuse(parents.dim() == 2 and parents.shape[0] >= 1 and parents.shape[1] >= 1, "parents must be [B, beam]")
+    B, beam = parents.shape
+    ptr = _array(parents, "parents", torch.int32, (B, beam), parents.device)
+    _refuse(lead in (0, 1), "lead must be 0 or 1")
+    _refuse(len(states) <= 16, "at most 16 tensors")
+    views = (_States * max(len(states), 1))()
+    for i, (v, t) in enumerate(zip(views, states)):
+        _refuse(t.device == parents.device, f"state {i} is on {t.device}, not on {parents.device}")
+        _refuse(t.dim() >= lead + 2 and tuple(t.shape[lead:lead + 2]) == (B, beam), f"state {i} must be [{'layers, ' * lead}B, beam, ...]")
+        shape, strides, size = t.shape, t.stride(), t.element_size()
+        rows, stride, run = _rows_of(shape[lead + 2:], strides[lead + 2:], f"state {i}")
+        v.data = t.data_ptr()
+        v.lead, v.lead_stride = (shape[0], strides[0] * size) if lead else (1, 0)
+        v.b_stride, v.slot_stride = strides[lead] * size, strides[lead + 1] * size
+        v.inner, v.inner_stride, v.row_bytes = rows, stride * size, run * size
+    with _Call(parents, stream, (parents, *states)) as raw:
+        _check(load_library().rnnt_reorder_states(C.c_void_p(ptr), B, beam, views, len(states), raw))
+
+
+class KVCache:
+    """The paged cache of one attention layer (rnnt_cache_t): ``k`` and ``v`` [n_pages, heads, page_size, dim], torch.float8_e4m3fn
+    (format "e4m3") or torch.float16 ("f16"), ``k_exp`` and ``v_exp`` uint8 [n_pages, heads, page_size]; a row's values are
+    k 2^(k_exp - 127).  Which pages belong to a sequence is the caller's to say, by a table int32 [B, width] with each call.  Sequences may
+    share pages, hypotheses of a beam those of their common prefix; with pages of one token a table lists each hypothesis' tokens."""
+
+    def __init__(self, n_pages, page_size, heads, dim, format="e4m3", device="cuda:0"):
+        import torch
+        _refuse(format in _FORMATS, "format must be 'e4m3' or 'f16'")
+        dtype = torch.float16 if format == "f16" else torch.float8_e4m3fn
+        shape = (n_pages, heads, page_size)
+        # (zeros that are written as bytes: a row that was never written reads as zeros)
+        k, v = (torch.zeros(shape + (dim * (2 if format == "f16" else 1),), dtype=torch.uint8, device=device).view(dtype) for _ in range(2))
+        self._set(k, v, torch.full(shape, 127, dtype=torch.uint8, device=device), torch.full(shape, 127, dtype=torch.uint8, device=device))
+
+    @classmethod
+    def from_tensors(cls, k, v, k_exp, v_exp):
+        """A cache over arrays that the caller holds."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_exp, v_exp)
+        return self
+
+    def _set(self, k, v, k_exp, v_exp):
+        import torch
+        _refuse(k.dim() == 4 and k.dtype in (torch.float16, torch.float8_e4m3fn), "k must be [n_pages, heads, page_size, dim], float8_e4m3fn or float16")
+        _refuse(k.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
+        self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
+        self.n_pages, self.heads, self.page_size, self.dim = k.shape
+        self.format = "f16" if k.dtype == torch.float16 else "e4m3"
+        self._c = _Cache(struct_size=C.sizeof(_Cache), format=_FORMATS[self.format], n_pages=self.n_pages, page_size=self.page_size,
+                         heads=self.heads, dim=self.dim)
+        self._c.k = _array(k, "k", k.dtype, tuple(k.shape), self.device)
+        self._c.v = _array(v, "v", k.dtype, tuple(k.shape), self.device)
+        self._c.k_exp = _array(k_exp, "k_exp", torch.uint8, tuple(k.shape[:3]), self.device)
+        self._c.v_exp = _array(v_exp, "v_exp", torch.uint8, tuple(k.shape[:3]), self.device)
+
+    def _view(self, table, B):
+        import torch
+        _refuse(table.dim() == 2 and table.dtype == torch.int32 and table.shape[0] == B and table.shape[1] >= 1, f"table must be int32 [{B}, width]")
+        _refuse(table.device == self.device, f"table is on {table.device}, not on {self.device}")
+        _refuse(table.shape[1] == 1 or table.stride(1) == 1, "rows of table must be contiguous")
+        c = _Cache.from_buffer_copy(self._c)
+        c.table, c.table_stride, c.width = table.data_ptr(), table.stride(0), table.shape[1]
+        return c
+
+    def _rows(self, t, what, heads):
+        _refuse(t.dim() == 4 and t.shape[2] == heads and t.shape[3] == self.dim, f"{what} must be [B, n, {heads}, {self.dim}]")
+        _refuse(t.device == self.device, f"{what} is on {t.device}, not on {self.device}")
+        _refuse(t.stride(3) == 1, f"the last dimension of {what} must be contiguous")
+        return _Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+    def _counts(self, start, count, B):
+        import torch
+        return (C.c_void_p(_array(start, "start", torch.int32, (B,), self.device)),
+                C.c_void_p(_array(count, "count", torch.int32, (B,), self.device)) if count is not None else None)
+
+    def write(self, k, v, table, start, count=None, stream=None):
+        """rnnt_cache_write: rows k, v [B, n, heads, dim] (float32, float16 or bfloat16) to positions start[b] + i, i < count[b] (None: n)."""
+        B, n = k.shape[:2]
+        _refuse(k.dtype == v.dtype and k.shape == v.shape, "k and v must have one type and shape")
+        code, c = _type_of(k, "k"), self._view(table, B)
+        rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
+        first, many = self._counts(start, count, B)
+        with _Call(k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp)) as raw:
+            _check(load_library().rnnt_cache_write(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+
+    def read(self, table, start, n, dtype=None, count=None, stream=None):
+        """rnnt_cache_read: (k, v) [B, n, heads, dim] of ``dtype`` (default float32), the rows at positions start[b] + i; zeros from count[b] on and
+        where there is no page."""
+        import torch
+        dtype = dtype or torch.float32
+        B = table.shape[0]
+        c = self._view(table, B)
+        first, many = self._counts(start, count, B)
+        with _Call(self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp)) as raw:
+            out = tuple(torch.empty((B, n, self.heads, self.dim), dtype=dtype, device=self.device) for _ in range(2))
+            if n:
+                code, rk, rv = _type_of(out[0], "dtype"), self._rows(out[0], "k", self.heads), self._rows(out[1], "v", self.heads)
+                _check(load_library().rnnt_cache_read(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+        return out
+
+    def attend(self, q, table, lens, parents=None, scale=None, max_len=None, out=None, stream=None):
+        """rnnt_cache_attend: attention of queries q [B, n, q_heads, dim] over lens[b] tokens (int32 [B]) and the new nodes behind them, whose
+        rows have been written to positions lens[b] + i.  ``parents`` int32 [B, tree], tree >= n: the queries are the last n nodes of a tree,
+        each sees its ancestors (-1: none) and itself; less than -1: padding.  None: each node follows the one before it, n = 1 is a step of
+        a search.  ``scale``: default dim ** -0.5.  ``max_len``: a bound of lens + tree, by which work is split (default: all that
+        the table holds).  Returns [B, n, q_heads, dim] of q's type; ``out``: contiguous, such a tensor to write to."""
+        import torch
+        _refuse(q.dim() == 4, "q must be [B, n, q_heads, dim]")
+        B, n, heads, dim = q.shape
+        c = self._view(table, B)
+        a = _Attend(struct_size=C.sizeof(_Attend), type=_type_of(q, "q"), B=B, n=n, tree=n, q_heads=heads,
+                    scale=dim ** -0.5 if scale is None else scale)
+        a.q = self._rows(q, "q", heads)
+        a.max_len = min(self.page_size * table.shape[1] if max_len is None else max_len, 0x7fffffff)
+        a.lens = _array(lens, "lens", torch.int32, (B,), self.device)
+        if parents is not None:
+            _refuse(parents.dim() == 2, "parents must be [B, tree]")
+            a.tree = parents.shape[1]
+            a.parents = _array(parents, "parents", torch.int32, (B, a.tree), self.device)
+        lib = load_library()
+        with _Call(q, stream, (q, table, lens, parents, out, self.k, self.v, self.k_exp, self.v_exp)) as raw:
+            a.workspace_bytes = _check(lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(a)))
+            if out is None:
+                out = torch.empty((B, n, heads, dim), dtype=q.dtype, device=self.device)
+                a.out = out.data_ptr()
+            else:
+                a.out = _array(out, "out", q.dtype, (B, n, heads, dim), self.device)
+            if a.workspace_bytes:
+                work = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
+                a.workspace = work.data_ptr()
+            _check(lib.rnnt_cache_attend(C.byref(c), C.byref(a), raw))
+        return out
+
+
+def nbest_tree(tokens, lens, max_nodes=None) -> dict:
+    """rnnt_nbest_tree: the prefix trees of the n-best lists of BeamDecoder.results (tokens [B, beam, cap], lens [B, beam], numpy), to be
+    rescored by one KVCache.attend: tokens and parents [B, nodes] (parent -1: first token, -2: padding), leaf [B, beam]: the node at which each
+    hypothesis ends (-1: empty), n_nodes [B]."""
+    tokens, lens = np.ascontiguousarray(tokens, np.int32), np.ascontiguousarray(lens, np.int32)
+    _refuse(tokens.ndim == 3 and lens.shape == tokens.shape[:2], "tokens must be [B, beam, cap], lens [B, beam]")
+    B, beam, cap = tokens.shape
+    room = max(1, int(np.maximum(lens, 0).sum(1).max(initial=0))) if max_nodes is None else max_nodes
+    tok, par = (np.empty((B, room), np.int32) for _ in range(2))
+    leaf, n_nodes = np.empty((B, beam), np.int32), np.empty(B, np.int32)
+    most = _check(load_library().rnnt_nbest_tree(*(C.c_void_p(x.ctypes.data) for x in (tokens, lens)), B, beam, cap, room,
+                                                 *(C.c_void_p(x.ctypes.data) for x in (tok, par, leaf, n_nodes))))
+    width = max(1, most) if max_nodes is None else max_nodes
+    return dict(tokens=np.ascontiguousarray(tok[:, :width]), parents=np.ascontiguousarray(par[:, :width]), leaf=leaf, n_nodes=n_nodes)

@@ -1,0 +1,224 @@
+"""Operators for networks that the caller runs itself, without a GPU: the prefix tree of n-best lists, what the host refuses (before any
+launch; the pointers below are never read), the plain implementations the GPU tests compare with."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import token_ref as R
+
+E_ARG = -1
+FAKE = 1 << 20  # an aligned address that nothing reads
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2506_00185_amd import binding, build
+    import os
+    if not os.path.exists(binding.library_path()):
+        build.build()
+    return binding.load_library()
+
+
+def message(lib):
+    return lib.rnnt_beam_last_error(None).decode()
+
+
+# ---------------------------------------------------------------- prefix trees
+def brute_tree(tokens, lens):
+    nodes, leaf = {}, []
+    for t, n in zip(tokens, lens):
+        for i in range(1, n + 1):
+            nodes.setdefault(tuple(t[:i]), len(nodes))
+        leaf.append(nodes[tuple(t[:n])] if n > 0 else -1)
+    return [p[-1] for p in nodes], [nodes.get(p[:-1], -1) for p in nodes], leaf
+
+
+@pytest.mark.parametrize("B,beam,cap,V,seed", [(1, 1, 1, 2, 0), (3, 4, 9, 2, 1), (5, 12, 30, 3, 2), (2, 16, 7, 50, 3)])
+def test_prefix_trees_of_nbest_lists(B, beam, cap, V, seed):
+    from paper_2506_00185_amd import nbest_tree
+    g = np.random.default_rng(seed)
+    tokens = g.integers(0, V, (B, beam, cap)).astype(np.int32)
+    lens = g.integers(-1, cap + 1, (B, beam)).astype(np.int32)  # -1: empty slot, 0: empty transcript
+    t = nbest_tree(tokens, lens)
+    for b in range(B):
+        tok, par, leaf = brute_tree(tokens[b], lens[b])
+        n = t["n_nodes"][b]
+        assert n == len(tok)
+        np.testing.assert_array_equal(t["tokens"][b, :n], tok)
+        np.testing.assert_array_equal(t["parents"][b, :n], par)
+        assert np.all(t["parents"][b, n:] == -2)
+        np.testing.assert_array_equal(t["leaf"][b], leaf)
+    assert t["parents"].shape[1] == max(1, t["n_nodes"].max())
+
+
+def test_prefix_tree_that_does_not_fit_is_refused():
+    from paper_2506_00185_amd import RnntBeamError, nbest_tree
+    tokens, lens = np.arange(6, dtype=np.int32).reshape(1, 2, 3), np.array([[3, 3]], np.int32)
+    assert nbest_tree(tokens, lens, max_nodes=6)["n_nodes"][0] == 6
+    with pytest.raises(RnntBeamError, match="max_nodes"):
+        nbest_tree(tokens, lens, max_nodes=5)
+    with pytest.raises(RnntBeamError, match="beyond cap"):
+        nbest_tree(tokens, lens + 1)
+
+
+# ---------------------------------------------------------------- refusals
+def a_select(**over):
+    from paper_2506_00185_amd.tokens import _Select
+    s = _Select(struct_size=C.sizeof(_Select), type=0, B=2, beam=4, V=100, eos=-1, logits=FAKE, stride_b=400, stride_k=100, scores=FAKE, done=None,
+                out_scores=FAKE, out_parent=FAKE, out_token=FAKE, out_done=None, workspace=FAKE, workspace_bytes=1 << 30)
+    for k, v in over.items():
+        setattr(s, k, v)
+    return s
+
+
+@pytest.mark.parametrize("over,what", [
+    (dict(struct_size=8), "struct_size"), (dict(type=3), "type"), (dict(type=-1), "type"), (dict(B=0), "B and V"), (dict(V=0), "B and V"), (dict(beam=0), "beam"),
+    (dict(beam=17), "beam"), (dict(beam=16, V=1 << 27), "2^31"), (dict(eos=100), "eos"), (dict(eos=-2), "eos"), (dict(eos=3), "out_done"),
+    (dict(done=FAKE), "done"), (dict(out_done=FAKE), "done"), (dict(logits=None), "NULL"), (dict(scores=None), "NULL"), (dict(out_token=None), "NULL"),
+    (dict(V=1 << 20, workspace=None), "workspace"), (dict(V=1 << 20, workspace_bytes=100), "workspace"), (dict(V=1 << 20, workspace=FAKE + 8), "workspace")])
+def test_selection_refuses(lib, over, what):
+    assert lib.rnnt_select_tokens(C.byref(a_select(**over)), None) == E_ARG
+    assert what in message(lib)
+
+
+def test_selection_workspace(lib):
+    assert lib.rnnt_select_tokens_workspace(1, 4, 1024) == 0
+    assert lib.rnnt_select_tokens_workspace(1, 4, 1 << 20) > 0
+    assert lib.rnnt_select_tokens_workspace(1, 17, 1 << 20) == 0
+    assert lib.rnnt_select_tokens(None, None) == E_ARG
+
+
+def a_state(**over):
+    from paper_2506_00185_amd.tokens import _States
+    s = _States(data=FAKE, lead_stride=0, b_stride=4000, slot_stride=1000, inner_stride=0, row_bytes=1000, lead=1, inner=1)
+    for k, v in over.items():
+        setattr(s, k, v)
+    return s
+
+
+@pytest.mark.parametrize("over,what", [
+    (dict(slot_stride=999), "overlap"), (dict(b_stride=3999), "overlap"), (dict(slot_stride=0), "overlap"), (dict(inner=2, inner_stride=500), "overlap"),
+    (dict(lead=2), "overlap"), (dict(slot_stride=-1000), "overlap"), (dict(row_bytes=-1), "negative"), (dict(inner=-1), "negative"), (dict(data=None), "NULL"),
+    (dict(row_bytes=1 << 50, slot_stride=1 << 50, b_stride=1 << 52), "more work")])
+def test_reordering_refuses(lib, over, what):
+    v = (type(a_state()) * 1)(a_state(**over))
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, v, 1, None) == E_ARG
+    assert what in message(lib)
+
+
+def test_reordering_refuses_counts_and_repeats(lib):
+    two = (type(a_state()) * 2)(a_state(), a_state())
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, two, 2, None) == E_ARG and "twice" in message(lib)
+    many = (type(a_state()) * 17)(*[a_state() for _ in range(17)])
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, many, 17, None) == E_ARG and "16" in message(lib)
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 17, two, 1, None) == E_ARG and "beam" in message(lib)
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 0, 4, two, 1, None) == E_ARG
+    assert lib.rnnt_reorder_states(None, 2, 4, two, 1, None) == E_ARG
+    # nothing to move: nothing is launched
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, None, 0, None) == 0
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 1, two, 1, None) == 0
+    empty = (type(a_state()) * 1)(a_state(row_bytes=0, data=None))
+    assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, empty, 1, None) == 0
+
+
+def a_cache(**over):
+    from paper_2506_00185_amd.tokens import _Cache
+    c = _Cache(struct_size=C.sizeof(_Cache), format=0, n_pages=10, page_size=16, heads=2, dim=64, k=FAKE, v=FAKE, k_exp=FAKE, v_exp=FAKE, table=FAKE,
+               table_stride=5, width=5)
+    for k, v in over.items():
+        setattr(c, k, v)
+    return c
+
+
+BAD_CACHES = [(dict(struct_size=1), "struct_size"), (dict(format=2), "format"), (dict(page_size=12), "page_size"), (dict(page_size=0), "page_size"),
+              (dict(page_size=8192), "page_size"), (dict(dim=0), "dim"), (dict(dim=72), "dim"), (dict(dim=272), "dim"), (dict(heads=0), "heads"), (dict(n_pages=0), "n_pages"),
+              (dict(width=0), "width"), (dict(k=FAKE + 8), "aligned"), (dict(v_exp=None), "NULL"), (dict(table=None), "NULL"),
+              (dict(n_pages=1 << 30, page_size=4096), "2^32"), (dict(width=1 << 30), "2^30")]
+
+
+@pytest.mark.parametrize("over,what", BAD_CACHES)
+def test_caches_that_are_refused(lib, over, what):
+    from paper_2506_00185_amd.tokens import _Rows
+    c, rows = a_cache(**over), _Rows(FAKE, 1, 1, 1)
+    for call in (lib.rnnt_cache_write, lib.rnnt_cache_read):
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 1, 1, C.c_void_p(FAKE), None, None) == E_ARG
+        assert what in message(lib)
+    assert lib.rnnt_cache_attend(C.byref(c), C.byref(an_attend()), None) == E_ARG and what in message(lib)
+    assert lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(an_attend())) == E_ARG
+
+
+def test_rows_that_are_refused(lib):
+    from paper_2506_00185_amd.tokens import _Rows
+    c, rows, none = a_cache(), _Rows(FAKE, 1, 1, 1), _Rows(None, 1, 1, 1)
+    for call in (lib.rnnt_cache_write, lib.rnnt_cache_read):
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 3, 1, 1, C.c_void_p(FAKE), None, None) == E_ARG and "type" in message(lib)
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 0, 1, C.c_void_p(FAKE), None, None) == E_ARG
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 1, -1, C.c_void_p(FAKE), None, None) == E_ARG
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 1, 1, None, None, None) == E_ARG
+        assert call(C.byref(c), C.byref(none), C.byref(rows), 0, 1, 1, C.c_void_p(FAKE), None, None) == E_ARG
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 1 << 30, 1 << 30, C.c_void_p(FAKE), None, None) == E_ARG and "more work" in message(lib)
+        assert call(C.byref(c), C.byref(rows), C.byref(rows), 0, 1, 0, C.c_void_p(FAKE), None, None) == 0  # no rows
+
+
+def an_attend(**over):
+    from paper_2506_00185_amd.tokens import _Attend, _Rows
+    a = _Attend(struct_size=C.sizeof(_Attend), type=0, B=2, n=3, tree=3, q_heads=4, scale=1.0, max_len=80, q=_Rows(FAKE, 1, 1, 1), out=FAKE, lens=FAKE,
+                parents=None, workspace=FAKE, workspace_bytes=1 << 30)
+    for k, v in over.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("over,what", [
+    (dict(struct_size=4), "struct_size"), (dict(type=7), "type"), (dict(B=0), "at least 1"), (dict(n=0), "at least 1"), (dict(tree=2), "tree"),
+    (dict(parents=FAKE, tree=1025), "1024"), (dict(q_heads=3), "q_heads"), (dict(q_heads=0), "q_heads"), (dict(max_len=-1), "max_len"), (dict(out=None), "NULL"),
+    (dict(lens=None), "NULL"), (dict(n=1 << 30, tree=1 << 30), "more work"), (dict(B=1 << 30), "more work")])
+def test_attention_refuses(lib, over, what):
+    assert lib.rnnt_cache_attend(C.byref(a_cache()), C.byref(an_attend(**over)), None) == E_ARG
+    assert what in message(lib)
+
+
+def test_attention_workspace(lib):
+    long = a_cache(n_pages=1000, width=1000)
+    need = lib.rnnt_cache_attend_workspace(C.byref(long), C.byref(an_attend(max_len=16000)))
+    assert need > 0
+    for over in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=FAKE + 4)):
+        assert lib.rnnt_cache_attend(C.byref(long), C.byref(an_attend(max_len=16000, **over)), None) == E_ARG and "workspace" in message(lib)
+
+
+def test_python_side_refuses_host_tensors():
+    import torch
+    from paper_2506_00185_amd import KVCache, RnntBeamError, reorder_states, select_tokens
+    with pytest.raises(RnntBeamError, match="GPU"):
+        select_tokens(torch.zeros(1, 2, 8), torch.zeros(1, 2, dtype=torch.float64))
+    with pytest.raises(RnntBeamError, match="GPU"):
+        reorder_states(torch.zeros(1, 2, dtype=torch.int32), [torch.zeros(1, 2, 3)])
+    with pytest.raises(RnntBeamError, match="GPU"):
+        KVCache(1, 16, 1, 64, device="cpu")
+
+
+# ---------------------------------------------------------------- the plain implementations themselves
+def test_plain_formats():
+    import torch
+    g = np.random.default_rng(0)
+    for fmt, dtype, top in (("e4m3", torch.float8_e4m3fn, 448.0), ("f16", torch.float16, 2.0**15)):
+        for e in (-140, -126, -20, 0, 5, 127):
+            x = np.float32(g.standard_normal(64) * 2.0**e) if e < 127 else np.float32(g.uniform(-3.4e38, 3.4e38, 64))
+            y, b = R.quantise(x, fmt)
+            assert np.abs(y).max() <= top
+            assert b == 1 or np.abs(y).max() > top / 2 - 2.0**9 * (fmt == "f16") - 16
+            np.testing.assert_array_equal(torch.from_numpy(y).float().to(dtype).double().numpy(), y)  # representable
+            np.testing.assert_array_equal(torch.ldexp(torch.from_numpy(x).double(), torch.tensor(127 - b)).float().to(dtype).double().numpy(), y)
+        assert R.quantise(np.array([448.0, 1.0]), "e4m3")[1] == 127 and R.quantise(np.array([449.0, 1.0]), "e4m3")[1] == 128
+        assert R.quantise(np.zeros(4), fmt)[1] == 127 and R.quantise(np.array([1.0, math.nan]), fmt)[1] == 255
+
+
+def test_plain_selection_and_paths():
+    s, p, t, d = R.select(np.log(np.array([[[0.5, 0.25, 0.25], [0.1, 0.8, 0.1]]])), np.array([[0.0, -0.1]]), eos=1)
+    np.testing.assert_array_equal(p, [[1, 0]])
+    np.testing.assert_array_equal(t, [[1, 0]])
+    np.testing.assert_allclose(s, [[-0.1 + math.log(0.8), math.log(0.5)]], rtol=1e-12)
+    np.testing.assert_array_equal(d, [[True, False]])
+    assert R.path_of([-1, 0, 0, 1], 3) == [3, 1, 0] and R.path_of([-1, -2, 1], 2) is None and R.path_of([0], 0) is None
