@@ -98,10 +98,10 @@ int attend_plan(const CacheView &c, const rnnt_attend_t *s, AttendPlan &p) {
   p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
   p.mt = rows > 16 && p.dp < 256 ? 2 : 1;
   p.row_tiles = (int)((rows + 16 * p.mt - 1) / (16 * p.mt));
-  // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for four on every unit, none shorter
+  // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for two on every unit, none shorter
   // than 256 tokens, two tiles for each of its waves
   const int64_t room = (int64_t)c.width << c.page_shift, longest = s->max_len < room ? (s->max_len > 1 ? s->max_len : 1) : room;
-  const int64_t others = pairs * p.row_tiles, want = (4 * kUnits + others - 1) / others, most = (longest + 255) / 256;
+  const int64_t others = pairs * p.row_tiles, want = (2 * kUnits + others - 1) / others, most = (longest + 255) / 256;
   int64_t splits = want < most ? want : most;
   int64_t len = ((longest + splits - 1) / splits + 127) / 128 * 128;
   splits = (longest + len - 1) / len;

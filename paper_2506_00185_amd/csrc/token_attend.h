@@ -7,8 +7,8 @@ namespace rb {
 // A block takes MT * 16 rows, a row being one query head of one node: the nodes of a sequence and the query heads that share a key head
 // side by side, so that a tree's nodes and the heads of a group fill a tile and the cache is read once for all of them.  Its four waves
 // take tiles of 32 tokens in turn; nothing goes through LDS but the tiles' exponents and row indices:
-//   S^T = K Q^T   a lane loads a quarter of a key row as it lies in memory, the matrix instruction's 8-k slices being cut
-//                 from those quarters (Q is held in the same order); it gets the logits of 4 + 4 tokens for one row,
+//   S^T = K Q^T   a lane loads every fourth 16 bytes of a key row as they lie in memory, the matrix instruction's 8-k slices being cut
+//                 from those (Q is held in the same order); it gets the logits of 4 + 4 tokens for one row,
 //   O^T = V^T P^T exactly which it hands back as the operand, again in an order of its own: k-slice j of lane group g is token 4 g + j
 //                 of the first 16 and of the second.  V^T's operand are the same tokens' values of dim / 16 neighbouring dims, which a
 //                 lane loads as they lie in memory and transposes in registers.
@@ -43,11 +43,15 @@ __device__ __forceinline__ uint32_t e4m3_hi(uint32_t w) { return __builtin_bit_c
 
 // Value exponents are taken relative to one of the sequence's first rows, so that the sums of a block stay far from float32's ends: the first that
 // tells anything (zero rows have kExpZero).  One call per wave; the same for all blocks of a sequence's head.
-__device__ __forceinline__ int reference_exp(const CacheView &c, int b, int h, int total) {
+__device__ __forceinline__ int reference_page(const CacheView &c, int b) {  // of the lane's token, the lane-th
+  return c.table[b * c.table_stride + min((int)(threadIdx.x & 63) >> c.page_shift, c.width - 1)];
+}
+__device__ __forceinline__ int reference_exp(const CacheView &c, int h, int page, int total) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = lane < total ? cache_row(c, b, lane, h) : -1;
-  const int e = row >= 0 ? c.v_exp[row] : kExpNaN;
-  const uint64_t good = __ballot(e != kExpZero && e != kExpNaN);
+  const bool there = lane < total && (unsigned)page < (unsigned)c.n_pages;
+  const uint32_t row = there ? (((uint32_t)page * c.heads + h) << c.page_shift) + (lane & (c.page_size - 1)) : 0u;
+  const int e = c.v_exp[row];
+  const uint64_t good = __ballot(there && e != kExpZero && e != kExpNaN);
   return good ? __builtin_amdgcn_readlane(e, __ffsll((unsigned long long)good) - 1) : kExpZero;
 }
 
@@ -98,23 +102,33 @@ struct Attend {
   static constexpr int QN = Q2 ? 2 : 1;
 
   struct Shared {
-    uint32_t mask[MT * 16][kTreeMax / 32];
+    union {
+      struct {
+        uint4 q[MT][QN][KS][64];  // operands of Q K, by lane
+        uint32_t mask[MT * 16][kTreeMax / 32];
+        int parents[kTreeMax];
+      };
+      float o[4][MT * 16][DP + 4];  // the waves' sums, when all have multiplied their last tile
+    };
     float m[4][MT * 16], l[4][MT * 16];
-    float o[4][MT * 16][DP + 4];
+    float q_scale[MT * 16];
     uint8_t gone[MT * 16];
   };
   struct Meta {  // of a wave's tile of 32 tokens
     uint32_t row[32];
     float k_scale[32], v_exp[32], v_inv[32];
   };
-  struct Tile {
-    Bytes<KQ * FB> k[2];
-    Bytes<VN * FB> v[8];
-  };
+  // a lane's part of a tile: key rows l16 and 16 + l16, and its dims of eight value rows
+  typedef Bytes<KQ * FB> Keys[2];
+  typedef Bytes<VN * FB> Values[8];
+  // Tiles in registers: two, one on its way while the other is multiplied, where they are small enough for two blocks of a unit; else one, whose
+  // keys are followed by the next ones when they have been multiplied, and its values likewise.
+  static constexpr int BUFS = DP * FB <= 64 ? 2 : 1;
+  static constexpr int WAVES = DP == 64 && MT == 1 ? (FMT == 8 ? 4 : 3) : DP == 128 && MT == 1 && FMT == 8 ? 3 : 2;
 };
 
 template <typename TT, int FMT, int DP, int MT>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_attend(AttendArgs a) {
   using A = Attend<TT, FMT, DP, MT>;
   typedef typename A::T T;
   constexpr int KS = A::KS, KQ = A::KQ, VN = A::VN, FB = A::FB, QN = A::QN;
@@ -123,13 +137,35 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
   const CacheView &c = a.c;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
 
-  // blocks of the same tokens on one XCD, one after the other: block i runs on XCD i % 8
+  // Blocks of the same tokens on one XCD, one after the other (block i runs on XCD i % 8); first splits first: which of the later ones have work
+  // hangs on the lengths, and with the splits of a sequence side by side some XCDs had those that do not (32 sequences of 1000 to 8000 tokens: 78 us)
   const int groups = a.B * c.heads * a.splits;
   const int per = 8 * a.row_tiles, slab = blockIdx.x / per, in = blockIdx.x - slab * per;
   const int item = slab * 8 + (in & 7), tile_r = in >> 3;
   if (item >= groups) return;
-  const int split = item % a.splits, bh = item / a.splits, b = bh / c.heads, h = bh - b * c.heads;
+  const int pairs = a.B * c.heads, split = item / pairs, bh = item - split * pairs, b = bh / c.heads, h = bh - b * c.heads;
   const int row0 = tile_r * MT * 16;
+
+  // ---- Q (a wave one tile's), parents and the first tokens' pages hang on nothing and leave first: a block begins with a chain of dependent
+  // loads, lengths -> pages -> rows, of one to two microseconds each, and is otherwise a few times that long
+  const int D = c.dim, q_tile = wave % MT;
+  // lane (l16, g4) takes of row l16 of a tile what a key row has in its bytes 64 j + 16 g4 .. + 16
+  const auto dim_of = [&](int s) { return FMT == 8 ? (s >> 1) * 64 + g4 * 16 + (s & 1) * 8 : s * 32 + g4 * 8; };
+  T raw[KS][8];
+  {
+    const int r = row0 + q_tile * 16 + l16, node = r / a.group, head = h * a.group + r % a.group;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bool there = r < a.rows && dim_of(s) < D;
+      const T *p = static_cast<const T *>(a.q) + (there ? b * a.stride_b + node * a.stride_n + head * a.stride_h + dim_of(s) : 0);
+      __builtin_memcpy(raw[s], p, sizeof(raw[s]));  // (the first row of all where there is none)
+    }
+  }
+  int parent[kTreeMax / 256] = {};
+  if (a.parents)
+#pragma unroll
+    for (int i = 0; i < kTreeMax / 256; ++i) parent[i] = a.parents[(int64_t)b * a.tree + min(i * 256 + (int)threadIdx.x, a.tree - 1)];
+  const int ref_page = reference_page(c, b);
 
   const int64_t room = (int64_t)c.width << c.page_shift;
   const int len = max(a.lens[b], 0);
@@ -137,78 +173,9 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
   const int t_begin = (int)min((int64_t)split * a.split_len, (int64_t)total);
   const int t_end = split + 1 < a.splits ? (int)min((int64_t)t_begin + a.split_len, (int64_t)total) : total;
   if (split && t_begin >= t_end) return;
-  const int D = c.dim;
 
-  // ---- which nodes a row sees, where the block's tokens reach into the tree
   const int first_q = a.tree - a.n;  // node of query 0
   const bool treed = a.parents && t_end > t_begin && (t_end > len || t_end == total);
-  if (treed) {
-    for (int i = threadIdx.x; i < MT * 16 * (kTreeMax / 32); i += 256) (&sh.mask[0][0])[i] = 0;
-    __syncthreads();
-    if (threadIdx.x < MT * 16) {
-      const int r = row0 + threadIdx.x;
-      bool gone = false;
-      if (r < a.rows) {
-        const int *parents = a.parents + (int64_t)b * a.tree;
-        int j = first_q + r / a.group;
-        while (true) {
-          sh.mask[threadIdx.x][j >> 5] |= 1u << (j & 31);
-          const int p = parents[j];
-          if (p < -1 || p >= j) {
-            gone = true;
-            break;
-          }
-          if (p < 0) break;
-          j = p;
-        }
-      }
-      sh.gone[threadIdx.x] = gone;
-    }
-    __syncthreads();
-  }
-
-  // ---- Q, in the order of the key rows: lane (l16, g4) holds values g4 KQ .. of row l16 of each tile
-  uintx4_t q[MT][QN][KS];
-  float q_scale[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int r = row0 + m * 16 + l16, node = r / a.group, head = h * a.group + r % a.group;
-    float x[KQ];
-    float most = 0.f;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < KQ; i += 8) {
-      const bool there = r < a.rows && g4 * KQ + i < D;
-      T raw[8] = {};
-      if (there) __builtin_memcpy(raw, static_cast<const T *>(a.q) + b * a.stride_b + node * a.stride_n + head * a.stride_h + g4 * KQ + i, sizeof(raw));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[i + j] = to_float(raw[j]);
-        most = fmaxf(most, fabsf(x[i + j]));
-        bad |= !(fabsf(x[i + j]) < INFINITY);
-      }
-    }
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    bad = bad || most == INFINITY;
-    bad = __shfl_xor((int)bad, 16) | (int)bad;
-    bad = __shfl_xor((int)bad, 32) | (int)bad;
-    // the row's largest to [2^14, 2^15)
-    const int e = min(max((int)(__float_as_uint(most) >> 23), 15), 254);
-    const float to = __uint_as_float((uint32_t)(min(254 + 14 - e, 254)) << 23);
-    const int back = 127 - (min(254 + 14 - e, 254) - 127);
-    q_scale[m] = bad ? NAN : __uint_as_float((uint32_t)max(back, 1) << 23) * a.scale * (float)kLog2E;
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float u = x[s * 8 + 2 * w] * to, v = x[s * 8 + 2 * w + 1] * to;
-        if (bad) u = v = 0.f;
-        const uint32_t hi = pack_f16(u, v);
-        q[m][0][s][w] = hi;
-        if constexpr (A::Q2) q[m][1][s][w] = pack_f16_rest(u, v, hi);
-      }
-  }
 
   floatx4 acc[MT][VN];
   float M[MT], sum[MT];
@@ -220,174 +187,210 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
     for (int i = 0; i < VN; ++i) acc[m][i] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int e0 = reference_exp(c, b, h, total);
-
-  typename A::Tile tile;
   typename A::Meta &mt = meta[wave];
-  // page of the lane's token of a tile: lanes 0..31 and 32..63 the same tokens
-  auto page_of = [&](int t0) {
-    const int t = t0 + (lane & 31);
-    return t < t_end ? c.table[b * c.table_stride + (t >> c.page_shift)] : -1;
-  };
-  // lanes 0..31: row of its token, and the exponent of K's row; 32..63: of V's
-  struct Head {
+  // Where a lane's part of a row lies: a lane whose dims a row does not have reads the first ones, against zeros of Q or for nothing.
+  int k_off[KQ * FB / 16];
+#pragma unroll
+  for (int j = 0; j < KQ * FB / 16; ++j) k_off[j] = 64 * j + 16 * g4 < D * FB ? 64 * j + 16 * g4 : 0;
+  const int v_off = l16 * VN < D ? l16 * VN * FB : 0, row_bytes = D * FB;
+  // Loads are never left out: those of tokens that are not there read row 0 of the cache.  A load behind a branch would make every wait one for all
+  // loads under way, the next tile's among them.
+  struct Head {  // lanes 0..31 and 32..63: the 32 tokens of a tile; row, exponent of K's row (lanes 32..63: of V's)
     uint32_t row;
     int e;
     bool there;
   };
+  auto page_of = [&](int t0) { return c.table[b * c.table_stride + (min(t0 + (lane & 31), t_end - 1) >> c.page_shift)]; };
+  const uint8_t *exps = lane < 32 ? c.k_exp : c.v_exp;
+  // row indices of a tile, for load_keys and load_values behind it
   auto head_of = [&](int t0, int page) {
     Head o;
     const int t = t0 + (lane & 31);
-    o.there = (unsigned)page < (unsigned)c.n_pages;
-    o.row = o.there ? (((uint32_t)page * c.heads + h) << c.page_shift) + (t & (c.page_size - 1)) : 0xffffffffu;
-    o.e = o.there ? (lane < 32 ? c.k_exp : c.v_exp)[o.row] : 0;
-    return o;
-  };
-  auto put_rows = [&](const Head &o) {
+    o.there = t < t_end && (unsigned)page < (unsigned)c.n_pages;
+    o.row = o.there ? (((uint32_t)page * c.heads + h) << c.page_shift) + (t & (c.page_size - 1)) : 0u;
     wave_lds_order();
     if (lane < 32) mt.row[lane] = o.row;
     wave_lds_order();
+    o.e = exps[o.row];
+    return o;
   };
-  auto load_tile = [&]() {
+  auto load_keys = [&](typename A::Keys &keys) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t row = mt.row[16 * i + l16];
-      const char *p = c.k + ((uint64_t)row * D + g4 * KQ) * FB;
+      const char *p = c.k + (uint64_t)mt.row[16 * i + l16] * (uint32_t)row_bytes;
 #pragma unroll
       for (int j = 0; j < KQ * FB / 16; ++j) {
-        Bytes<16> part = {};
-        if (row != 0xffffffffu && g4 * KQ + j * 16 / FB < D) load_bytes(part, p + 16 * j);
+        Bytes<16> part;
+        load_bytes(part, p + k_off[j]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) tile.k[i].w[4 * j + w] = part.w[w];
+        for (int w = 0; w < 4; ++w) keys[i].w[4 * j + w] = part.w[w];
       }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t row = mt.row[(j >> 2) * 16 + 4 * g4 + (j & 3)];
-      const char *p = c.v + ((uint64_t)row * D + l16 * VN) * FB;
-      tile.v[j] = {};
-      if (row != 0xffffffffu && l16 * VN < D) load_bytes(tile.v[j], p);
     }
   };
+  auto load_values = [&](typename A::Values &values) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) load_bytes(values[j], c.v + (uint64_t)mt.row[(j >> 2) * 16 + 4 * g4 + (j & 3)] * (uint32_t)row_bytes + v_off);
+  };
 
+  // ---- the first tile's loads leave ahead of everything that does not need them
   int t0 = t_begin + wave * 32;
-  Head head = {};
-  int page_next = -1;
-  if (t0 < t_end) {
-    head = head_of(t0, page_of(t0));
-    put_rows(head);
-    load_tile();
+  const bool busy = t0 < t_end;
+  typename A::Keys keys[A::BUFS];
+  typename A::Values values[A::BUFS];
+  Head head[2] = {};
+  int page_next = 0;
+  if (busy) {
+    const int page = page_of(t0);
     page_next = page_of(t0 + 128);
+    head[0] = head_of(t0, page);
+    load_keys(keys[0]);
+    load_values(values[0]);
   }
-  for (; t0 < t_end; t0 += 128) {
-    // exponents of this tile
-    {
-      const bool nan = head.e == kExpNaN;
-      wave_lds_order();
-      if (lane < 32) {
-        mt.k_scale[lane] = !head.there ? 0.f : nan ? NAN : ldexpf(1.f, head.e - 127);
-      } else {
-        const int e = min(max(head.e - e0, -100), 100);
-        mt.v_exp[lane - 32] = !head.there ? -INFINITY : nan ? NAN : (float)e;
-        mt.v_inv[lane - 32] = !head.there ? 1.f : ldexpf(1.f, -e);
-      }
-      wave_lds_order();
-    }
-    if (__any(lane >= 32 && head.there && head.e == kExpZero)) {
-      // maybe a row of zeros, whose exponent says nothing about the others' and must not become the largest: 16 lanes hold its words
+  const int e0 = reference_exp(c, h, ref_page, total);
+
+  {
+    const int r = row0 + q_tile * 16 + l16;
+    float most = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bool there = r < a.rows && dim_of(s) < D;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        uint32_t any = 0;
+        if (!there) raw[s][j] = 0;
+        most = fmaxf(most, fabsf(to_float(raw[s][j])));
+        bad |= !(fabsf(to_float(raw[s][j])) < INFINITY);
+      }
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    bad = __shfl_xor((int)bad, 16) | (int)bad;
+    bad = __shfl_xor((int)bad, 32) | (int)bad;
+    // the row's largest to [2^14, 2^15)
+    const int e = min(max((int)(__float_as_uint(most) >> 23), 15), 254);
+    const float to = __uint_as_float((uint32_t)(268 - e) << 23);
+    if (g4 == 0 && wave < MT) sh.q_scale[q_tile * 16 + l16] = bad ? NAN : __uint_as_float((uint32_t)(e - 14) << 23) * a.scale * (float)kLog2E;
 #pragma unroll
-        for (int w = 0; w < VN * FB / 4; ++w) any |= tile.v[j].w[w] & (FMT == 8 ? 0x7f7f7f7fu : 0x7fff7fffu);
-        const uint64_t held = __ballot(any != 0);
-        const int t = (j >> 2) * 16 + 4 * g4 + (j & 3);
-        if (l16 == 0 && !(held >> (16 * g4) & 0xffff) && fabsf(mt.v_exp[t]) < INFINITY) {
-          mt.v_exp[t] = 0.f;
-          mt.v_inv[t] = 1.f;
+    for (int s = 0; s < KS; ++s) {
+      if (s % (4 / MT) != wave / MT) continue;  // the waves of a tile share its steps
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float u = bad ? 0.f : to_float(raw[s][2 * w]) * to, v = bad ? 0.f : to_float(raw[s][2 * w + 1]) * to;
+        hi[w] = pack_f16(u, v);
+        if constexpr (A::Q2) lo[w] = pack_f16_rest(u, v, hi[w]);
+      }
+      sh.q[q_tile][0][s][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      if constexpr (A::Q2) sh.q[q_tile][1][s][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+  }
+
+  // ---- which nodes a row sees, where the block's tokens reach into the tree
+  if (treed) {
+    // (the walk is a chain of dependent reads: through LDS)
+    const int words = (a.tree + 31) >> 5;
+    for (int i = threadIdx.x; i < MT * 16 * words; i += 256) sh.mask[i / words][i % words] = 0;
+#pragma unroll
+    for (int i = 0; i < kTreeMax / 256; ++i) sh.parents[i * 256 + threadIdx.x] = parent[i];
+    __syncthreads();
+    if (threadIdx.x < MT * 16) {
+      const int r = row0 + threadIdx.x;
+      bool gone = false;
+      if (r < a.rows) {
+        int j = first_q + r / a.group;
+        while (true) {
+          sh.mask[threadIdx.x][j >> 5] |= 1u << (j & 31);
+          const int p = sh.parents[j];
+          if (p < -1 || p >= j) {
+            gone = true;
+            break;
+          }
+          if (p < 0) break;
+          j = p;
         }
+      }
+      sh.gone[threadIdx.x] = gone;
+    }
+  }
+  __syncthreads();
+  float q_scale[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) q_scale[m] = sh.q_scale[m * 16 + l16];
+
+  // one tile; `next_keys` and `next_values` are called when its registers may be written again
+  auto take_tile = [&](int t0, const Head &head, const typename A::Keys &keys, const typename A::Values &values, auto next_keys, auto next_values) {
+    // tiles that reach beyond the tokens kept before, or hold tokens that are not there
+    const bool careful = t0 + 32 > len || __any(!head.there);
+    {
+      const bool nan = head.e == kExpNaN;
+      const int e = min(max(head.e - e0, -100), 100);
+      wave_lds_order();
+      if (lane < 32) {
+        mt.k_scale[lane] = nan ? NAN : ldexpf(1.f, head.e - 127);
+      } else {
+        mt.v_exp[lane - 32] = !head.there ? -INFINITY : nan ? NAN : (float)e;
+        mt.v_inv[lane - 32] = ldexpf(1.f, -e);
       }
       wave_lds_order();
-    }
-    float ks[8], ve[8], vi[8];
+      if (__any(lane >= 32 && head.there && head.e == kExpZero)) {
+        // maybe a row of zeros, whose exponent says nothing about the others' and must not become the largest: 16 lanes hold its words
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 8; ++j) {
+          uint32_t any = 0;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        ks[4 * i + r] = mt.k_scale[16 * i + 4 * g4 + r];
-        ve[4 * i + r] = mt.v_exp[16 * i + 4 * g4 + r];
-        vi[4 * i + r] = mt.v_inv[16 * i + 4 * g4 + r];
-      }
-    // operands
-    uintx4_t ka[2][KS];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        if constexpr (FMT == 8) {
-          const uint32_t w0 = tile.k[i].w[2 * s], w1 = tile.k[i].w[2 * s + 1];
-          ka[i][s] = uintx4_t{e4m3_lo(w0), e4m3_hi(w0), e4m3_lo(w1), e4m3_hi(w1)};
-        } else {
-          ka[i][s] = uintx4_t{tile.k[i].w[4 * s], tile.k[i].w[4 * s + 1], tile.k[i].w[4 * s + 2], tile.k[i].w[4 * s + 3]};
+          for (int w = 0; w < VN * FB / 4; ++w) any |= values[j].w[w] & (FMT == 8 ? 0x7f7f7f7fu : 0x7fff7fffu);
+          const uint64_t held = __ballot(any != 0);
+          const int t = (j >> 2) * 16 + 4 * g4 + (j & 3);
+          if (l16 == 0 && !(held >> (16 * g4) & 0xffff) && fabsf(mt.v_exp[t]) < INFINITY) {
+            mt.v_exp[t] = 0.f;
+            mt.v_inv[t] = 1.f;
+          }
         }
-      }
-    uintx4_t va[VN];
-#pragma unroll
-    for (int jp = 0; jp < 4; ++jp) {
-#pragma unroll
-      for (int w = 0; w < VN * FB / 4; ++w) {
-        const uint32_t lo = tile.v[2 * jp].w[w], hi = tile.v[2 * jp + 1].w[w];
-        if constexpr (FMT == 8) {
-          const uint32_t p0 = perm_b32(hi, lo, 0x05010400u), p1 = perm_b32(hi, lo, 0x07030602u);
-          va[4 * w][jp] = e4m3_lo(p0);
-          va[4 * w + 1][jp] = e4m3_hi(p0);
-          va[4 * w + 2][jp] = e4m3_lo(p1);
-          va[4 * w + 3][jp] = e4m3_hi(p1);
-        } else {
-          va[2 * w][jp] = perm_b32(hi, lo, 0x05040100u);
-          va[2 * w + 1][jp] = perm_b32(hi, lo, 0x07060302u);
-        }
+        wave_lds_order();
       }
     }
-    const bool masked = t0 + 32 > len;
-    if (masked) {  // rows of padding, or of nodes that no query sees, hold anything: a p of zero must not meet a NaN or an infinity
+    floatx4 ks[2], ve[2], vi[2];
 #pragma unroll
-      for (int i = 0; i < VN; ++i)
-#pragma unroll
-        for (int jp = 0; jp < 4; ++jp) va[i][jp] = finite_f16(va[i][jp]);
+    for (int i = 0; i < 2; ++i) {
+      ks[i] = *reinterpret_cast<const floatx4 *>(&mt.k_scale[16 * i + 4 * g4]);
+      ve[i] = *reinterpret_cast<const floatx4 *>(&mt.v_exp[16 * i + 4 * g4]);
+      vi[i] = *reinterpret_cast<const floatx4 *>(&mt.v_inv[16 * i + 4 * g4]);
     }
-    // the next tile's loads leave before this one's products
-    Head head_next = {};
-    const int t_next = t0 + 128;
-    if (t_next < t_end) {
-      head_next = head_of(t_next, page_next);
-      put_rows(head_next);
-      load_tile();
-      page_next = page_of(t_next + 128);
-    }
+    floatx4 s[MT][2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      floatx4 s[2];
+    for (int m = 0; m < MT; ++m) s[m][0] = s[m][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        uintx4_t ka;
+        if constexpr (FMT == 8) {
+          const uint32_t w0 = keys[i].w[2 * k], w1 = keys[i].w[2 * k + 1];
+          ka = uintx4_t{e4m3_lo(w0), e4m3_hi(w0), e4m3_lo(w1), e4m3_hi(w1)};
+        } else {
+          ka = uintx4_t{keys[i].w[4 * k], keys[i].w[4 * k + 1], keys[i].w[4 * k + 2], keys[i].w[4 * k + 3]};
+        }
 #pragma unroll
-        for (int n = 0; n < QN; ++n)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int k = 0; k < KS; ++k) s[i] = mfma16_f16(ka[i][k], q[m][n][k], s[i]);
+          for (int n = 0; n < QN; ++n) s[m][i] = mfma16_f16(ka, __builtin_bit_cast(uintx4_t, sh.q[m][n][k][lane]), s[m][i]);
       }
+    next_keys();
+    uintx4_t pb[MT], pl[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
       float x[8];
       float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = fmaf(s[j >> 2][j & 3], ks[j] * q_scale[m], ve[j]);
-      if (masked) {
+      for (int j = 0; j < 8; ++j) x[j] = fmaf(s[m][j >> 2][j & 3], ks[j >> 2][j & 3] * q_scale[m], ve[j >> 2][j & 3]);
+      if (careful) {
         const int r = m * 16 + l16, node = first_q + (row0 + r) / a.group;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int at = t0 + (j >> 2) * 16 + 4 * g4 + (j & 3) - len;
           bool sees = at < 0;
           if (at >= 0 && at < a.tree) sees = a.parents ? (sh.mask[r][at >> 5] >> (at & 31)) & 1 : at <= node;
-          x[j] = sees ? x[j] : -INFINITY;
+          x[j] = sees && ve[j >> 2][j & 3] != -INFINITY ? x[j] : -INFINITY;
         }
       }
 #pragma unroll
@@ -406,25 +409,83 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         p[j] = __builtin_amdgcn_exp2f(x[j] - off);
-        sum[m] = fmaf(p[j], vi[j], sum[m]);
+        sum[m] = fmaf(p[j], vi[j >> 2][j & 3], sum[m]);
       }
-      uintx4_t pb, pl;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const uint32_t hi = pack_f16(p[2 * w], p[2 * w + 1]);
-        pb[w] = hi;
-        if constexpr (A::P2) pl[w] = pack_f16_rest(p[2 * w], p[2 * w + 1], hi);
-      }
-#pragma unroll
-      for (int i = 0; i < VN; ++i) {
-        acc[m][i] = mfma16_f16(va[i], pb, acc[m][i]);
-        if constexpr (A::P2) acc[m][i] = mfma16_f16(va[i], pl, acc[m][i]);
+        pb[m][w] = hi;
+        if constexpr (A::P2) pl[m][w] = pack_f16_rest(p[2 * w], p[2 * w + 1], hi);
       }
     }
-    head = head_next;
+    // four (two) dims at a time: the words of eight tokens that hold them, transposed
+#pragma unroll
+    for (int w = 0; w < VN * FB / 4; ++w) {
+      constexpr int PER = 4 / FB;
+      uintx4_t va[PER];
+#pragma unroll
+      for (int jp = 0; jp < 4; ++jp) {
+        const uint32_t lo = values[2 * jp].w[w], hi = values[2 * jp + 1].w[w];
+        if constexpr (FMT == 8) {
+          const uint32_t p0 = perm_b32(hi, lo, 0x05010400u), p1 = perm_b32(hi, lo, 0x07030602u);
+          va[0][jp] = e4m3_lo(p0);
+          va[1][jp] = e4m3_hi(p0);
+          va[2][jp] = e4m3_lo(p1);
+          va[3][jp] = e4m3_hi(p1);
+        } else {
+          va[0][jp] = perm_b32(hi, lo, 0x05040100u);
+          va[1][jp] = perm_b32(hi, lo, 0x07060302u);
+        }
+      }
+      if (careful) {  // rows of padding, or of nodes that no query sees, hold anything: a p of zero must not meet a NaN or an infinity
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+          for (int jp = 0; jp < 4; ++jp) va[i][jp] = finite_f16(va[i][jp]);
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          acc[m][PER * w + i] = mfma16_f16(va[i], pb[m], acc[m][PER * w + i]);
+          if constexpr (A::P2) acc[m][PER * w + i] = mfma16_f16(va[i], pl[m], acc[m][PER * w + i]);
+        }
+    }
+    next_values();
+  };
+
+  if (busy) {
+    if constexpr (A::BUFS == 2) {
+      const auto nothing = [] {};
+      while (true) {
+        head[1] = head_of(t0 + 128, page_next);
+        load_keys(keys[1]);
+        load_values(values[1]);
+        page_next = page_of(t0 + 256);
+        take_tile(t0, head[0], keys[0], values[0], nothing, nothing);
+        t0 += 128;
+        if (t0 >= t_end) break;
+        head[0] = head_of(t0 + 128, page_next);
+        load_keys(keys[0]);
+        load_values(values[0]);
+        page_next = page_of(t0 + 256);
+        take_tile(t0, head[1], keys[1], values[1], nothing, nothing);
+        t0 += 128;
+        if (t0 >= t_end) break;
+      }
+    } else {
+      do {
+        head[1] = head_of(t0 + 128, page_next);
+        page_next = page_of(t0 + 256);
+        take_tile(t0, head[0], keys[0], values[0], [&] { load_keys(keys[0]); }, [&] { load_values(values[0]); });
+        head[0] = head[1];
+        t0 += 128;
+      } while (t0 < t_end);
+    }
   }
 
   // ---- the four waves' shares
+  __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     float l = sum[m];
@@ -474,19 +535,22 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a) {
   }
 }
 
-// ---- shares of the splits of a row: a block per 4 rows, a wave for each
+// ---- shares of the splits of a row: a block for each row, dim / 4 lanes for a share, as many shares at a time as the block has room for
 template <typename TT>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   typedef typename TT::T T;
+  __shared__ floatx4 sh_o[256];
+  __shared__ float sh_l;
   const CacheView &c = a.c;
-  const int lane = threadIdx.x & 63, D = c.dim;
-  const int64_t all = (int64_t)a.B * c.heads * a.rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= all) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = c.dim, lanes = D / 4, shares = 256 / lanes;
+  const int64_t all = (int64_t)a.B * c.heads * a.rows, at = blockIdx.x;
   const int bh = (int)(at / a.rows), row = (int)(at - (int64_t)bh * a.rows), b = bh / c.heads, h = bh - b * c.heads;
+  const int ref_page = reference_page(c, b);
   const int64_t room = (int64_t)c.width << c.page_shift;
   const int total = (int)min((int64_t)max(a.lens[b], 0) + a.tree, room);
-  const int e0 = reference_exp(c, b, h, total);
   const int used = min(a.splits, (total + a.split_len - 1) / a.split_len);
+  const int e0 = reference_exp(c, h, ref_page, total);
+  // every wave all of the maxima, their sum and its own shares' factors
   float m_all = kMStart, l = 0.f;
   bool gone = false;
   for (int s = lane; s < used; s += 64) {
@@ -495,24 +559,34 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     gone |= st.y < 0.f;
   }
   m_all = wave_max(m_all);
-  gone = __any(gone);
+  const int mine = threadIdx.x / lanes, d = threadIdx.x % lanes * 4;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  const int d = lane * 4;
-  if (!gone)
-    for (int s = 0; s < used; ++s) {
-      const float2 st = a.stat[s * all + at];
-      const float f = __builtin_amdgcn_exp2f(st.x - m_all);
-      l = fmaf(f, st.y, l);
-      if (d < D) o += f * *reinterpret_cast<const floatx4 *>(a.part + (s * all + at) * D + d);
+  if (mine < shares) {
+#pragma unroll 4
+    for (int s = mine; s < used; s += shares) {
+      const float f = __builtin_amdgcn_exp2f(a.stat[s * all + at].x - m_all);
+      o += f * *reinterpret_cast<const floatx4 *>(a.part + (s * all + at) * D + d);
     }
-  if (d >= D) return;
+  }
+  if (wave == 0) {
+    for (int s = lane; s < used; s += 64) {
+      const float2 st = a.stat[s * all + at];
+      l = fmaf(__builtin_amdgcn_exp2f(st.x - m_all), st.y, l);
+    }
+    l = __any(gone) ? 0.f : wave_sum(l);
+    if (lane == 0) sh_l = l;
+  }
+  sh_o[threadIdx.x] = o;
+  __syncthreads();
+  if (threadIdx.x >= lanes) return;
+  for (int s = 1; s < shares && s < used; ++s) o += sh_o[s * lanes + threadIdx.x];
+  l = sh_l;
   const int node = row / a.group, head_i = h * a.group + row % a.group;
   T *out = static_cast<T *>(a.out) + (((int64_t)b * a.n + node) * (c.heads * a.group) + head_i) * D + d;
-  const bool none = gone || l == 0.f;
   const float inv = 1.f / l, back = ldexpf(1.f, e0 - 127);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float y = none ? 0.f : o[j] * inv * back;
+    const float y = l == 0.f ? 0.f : o[j] * inv * back;
     if constexpr (std::is_same<T, uint16_t>::value) out[j] = (uint16_t)pack_bf16_rne(y, y);
     else out[j] = (T)y;
   }
