@@ -37,16 +37,25 @@ int cache_view(const rnnt_cache_t *c, CacheView &v) {
   return RNNT_OK;
 }
 
+template <typename TT, int FMT, bool WRITE, int LANES>
+int rows_lanes(RowsArgs &a, hipStream_t stream) {
+  constexpr int kRows = 256 / LANES;
+  const int rows = a.n * a.c.heads;
+  // four rows for a group of lanes where that leaves two blocks for every unit: loads of a block under way; else one, for more blocks
+  const bool four = (int64_t)a.B * ((rows + 4 * kRows - 1) / (4 * kRows)) * 2 >= 2 * kUnits;
+  a.blocks = (rows + kRows * (four ? 4 : 1) - 1) / (kRows * (four ? 4 : 1));
+  const int64_t blocks = (int64_t)a.B * a.blocks;
+  if constexpr (WRITE) return launch(four ? k_cache_write<TT, FMT, LANES, 4> : k_cache_write<TT, FMT, LANES, 1>, blocks, 2, 256, a, stream);
+  else return launch(four ? k_cache_read<TT, FMT, LANES, 4> : k_cache_read<TT, FMT, LANES, 1>, blocks, 2, 256, a, stream);
+}
 template <typename TT, int FMT, bool WRITE>
-int rows_typed(const RowsArgs &a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.B * a.n * a.c.heads;
+int rows_typed(RowsArgs &a, hipStream_t stream) {
   const int lanes = a.c.dim / 8;
-  auto go = [&](void (*kernel)(RowsArgs), int per) { return launch(kernel, (rows + 256 / per - 1) / (256 / per), 2, 256, a, stream); };
-  if (lanes <= 2) return go(WRITE ? k_cache_write<TT, FMT, 2> : k_cache_read<TT, FMT, 2>, 2);
-  if (lanes <= 4) return go(WRITE ? k_cache_write<TT, FMT, 4> : k_cache_read<TT, FMT, 4>, 4);
-  if (lanes <= 8) return go(WRITE ? k_cache_write<TT, FMT, 8> : k_cache_read<TT, FMT, 8>, 8);
-  if (lanes <= 16) return go(WRITE ? k_cache_write<TT, FMT, 16> : k_cache_read<TT, FMT, 16>, 16);
-  return go(WRITE ? k_cache_write<TT, FMT, 32> : k_cache_read<TT, FMT, 32>, 32);
+  if (lanes <= 2) return rows_lanes<TT, FMT, WRITE, 2>(a, stream);
+  if (lanes <= 4) return rows_lanes<TT, FMT, WRITE, 4>(a, stream);
+  if (lanes <= 8) return rows_lanes<TT, FMT, WRITE, 8>(a, stream);
+  if (lanes <= 16) return rows_lanes<TT, FMT, WRITE, 16>(a, stream);
+  return rows_lanes<TT, FMT, WRITE, 32>(a, stream);
 }
 
 template <bool WRITE>
@@ -58,7 +67,7 @@ int rows_call(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t
   if (B < 1 || n < 0) return refuse("B must be at least 1, n not negative");
   if (n == 0) return RNNT_OK;
   if (!k->data || !v->data) return refuse("NULL array");
-  if ((int64_t)B * n > 0x7fffffffll * 16 / a.c.heads) return refuse("more work than one launch takes");
+  if ((int64_t)n * a.c.heads > 1 << 30) return refuse("more work than one launch takes");
   const rnnt_rows_t *r[2] = {k, v};
   for (int i = 0; i < 2; ++i) {
     a.in[i] = r[i]->data;
@@ -71,6 +80,11 @@ int rows_call(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t
   a.count = count;
   a.B = B;
   a.n = n;
+  // x / heads = upper half of x mul, shifted: mul = 2^(31 + l) / heads + 1 for 2^(l - 1) < heads <= 2^l, exact for x below 2^31
+  int l = 0;
+  while ((1 << l) < a.c.heads && l < 30) ++l;
+  a.by_heads.shift = l - 1;
+  a.by_heads.mul = l ? (uint32_t)(((uint64_t)1 << (31 + l)) / (uint32_t)a.c.heads + 1) : 0;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const bool f8 = cache->format == RNNT_CACHE_E4M3;
   switch (type) {

@@ -33,15 +33,22 @@ SelectPlan select_plan(int B, int beam, int V) {
   if (parts < fill) parts = fill < fine ? fill : fine;
   p.parts = (int)(parts < most ? parts : most);
   p.part_len = (V + p.parts - 1) / p.parts;
-  p.part_len = (p.part_len + 31) / 32 * 32;  // four waves' parts, each a multiple of 16 bytes
   return p;
 }
 
 template <typename TT>
 int select_typed(const SelectArgs &a, bool one, hipStream_t stream) {
-  if (one) return launch(k_select_one<TT>, a.B, 1, 1024, a, stream);
-  const int rc = launch(k_select_scan<TT>, (int64_t)a.B * a.beam * a.parts, 1, 256, a, stream);
-  return rc ? rc : launch(k_select_join, a.B, 1, 256, a, stream);
+  // tiles no longer than the parts need: what a tile has beyond a part costs as much as what it has in it
+  constexpr int kVec = 16 / (int)sizeof(typename TT::T);
+  if (one) {
+    const int vecs = (a.part_len + 64 * kVec - 1) / (64 * kVec);
+    if (vecs <= 1) return launch(k_select_one<TT, 1>, a.B, 1, 1024, a, stream);
+    if (vecs <= 2 || kVec == 8) return launch(k_select_one<TT, 2>, a.B, 1, 1024, a, stream);
+    if constexpr (kVec == 4) return launch(k_select_one<TT, 4>, a.B, 1, 1024, a, stream);
+  }
+  const int64_t blocks = (int64_t)a.B * a.beam * a.parts;
+  const int rc = launch(a.part_len <= 2048 ? k_select_scan<TT, 8> : a.part_len <= 4096 ? k_select_scan<TT, 16> : k_select_scan<TT, 32>, blocks, 1, 256, a, stream);
+  return rc ? rc : launch(k_select_join, a.B, 1, 64, a, stream);
 }
 
 template <typename V>

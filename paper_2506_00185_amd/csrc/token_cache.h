@@ -29,13 +29,21 @@ __device__ __forceinline__ int64_t cache_row(const CacheView &c, int b, int64_t 
 }
 
 // ---- rows in and out of the cache
+// x / d for x below 2^31: the upper half of a product
+struct Divisor {
+  uint32_t mul;
+  int shift;  // -1: d = 1
+};
+__device__ __forceinline__ int divide(int x, Divisor d) { return d.shift < 0 ? x : (int)(__umulhi((uint32_t)x, d.mul) >> d.shift); }
+
 struct RowsArgs {
   CacheView c;
   const void *in[2];  // [B][n][heads][dim], strides in elements, dim contiguous
   void *out[2];
   int64_t stride_b[2], stride_n[2], stride_h[2];
   const int *start, *count;  // [B]; count may be NULL
-  int B, n;
+  int B, n, blocks;          // blocks of a sequence
+  Divisor by_heads;
 };
 
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
@@ -57,53 +65,69 @@ __device__ __forceinline__ uint32_t row_max_u(uint32_t v) {
   return v;
 }
 
-// 8 values of a row for each lane, LANES lanes (the power of two from dim / 8 on) for a row: its largest |x| stays in
-// registers, every byte is read and written once.  Bound by memory.
-template <typename TT, int FMT, int LANES>
+// 8 values of a row for each lane, LANES lanes (the power of two from dim / 8 on) for a row, U rows for each of their groups: a row's largest |x|
+// stays in registers, every byte is read and written once.  Bound by memory: a block's loads all leave at once.
+// The rows of a sequence are counted through its tokens' heads; `which`: keys or values.
+struct RowAt {
+  int i, h;
+  bool mine;  // a row of the call, and dims of it
+};
+template <int LANES>
+__device__ __forceinline__ RowAt row_at(const RowsArgs &a, int r) {
+  RowAt o;
+  o.i = divide(r, a.by_heads);
+  o.h = r - o.i * a.c.heads;
+  o.mine = r < a.n * a.c.heads && (int)(threadIdx.x % LANES) * 8 < a.c.dim;
+  return o;
+}
+
+template <typename TT, int FMT, int LANES, int U>
 __global__ __launch_bounds__(256) void k_cache_write(RowsArgs a) {
   typedef typename TT::T T;
   constexpr int ROWS = 256 / LANES;
-  const int which = blockIdx.y, l = threadIdx.x % LANES;
-  const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  const int heads = a.c.heads, dim = a.c.dim;
-  const int h = (int)(r % heads);
-  const int64_t bn = r / heads;
-  const int n = (int)(bn % a.n), b = (int)(bn / a.n);
-  int64_t row = -1;
-  if (b < a.B && !(a.count && n >= a.count[b])) row = cache_row(a.c, b, (int64_t)a.start[b] + n, h);
-  float x[8] = {};
-  uint32_t most = 0;
-  const bool mine = row >= 0 && l * 8 < dim;
-  if (mine) {
-    const T *p = static_cast<const T *>(a.in[which]) + b * a.stride_b[which] + n * a.stride_n[which] + h * a.stride_h[which] + l * 8;
-    T raw[8];
-    __builtin_memcpy(raw, p, sizeof(raw));
+  const int which = blockIdx.y, l = threadIdx.x % LANES, b = blockIdx.x / a.blocks, dim = a.c.dim;
+  const int r0 = (blockIdx.x - b * a.blocks) * ROWS * U + threadIdx.x / LANES;
+  const int start = a.start[b], count = a.count ? a.count[b] : a.n;
+  const T *in = static_cast<const T *>(a.in[which]) + b * a.stride_b[which] + l * 8;
+  T raw[U][8];
+  int64_t row[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const RowAt at = row_at<LANES>(a, r0 + u * ROWS);
+    __builtin_memcpy(raw[u], at.mine ? in + at.i * a.stride_n[which] + at.h * a.stride_h[which] : static_cast<const T *>(a.in[which]), sizeof(raw[u]));
+    row[u] = at.mine && at.i < count ? cache_row(a.c, b, (int64_t)start + at.i, at.h) : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float x[8];
+    uint32_t most = 0;
+    const bool mine = row_at<LANES>(a, r0 + u * ROWS).mine;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      x[j] = to_float(raw[j]);
+      x[j] = to_float(raw[u][j]);
       most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);  // (of infinities and NaN the largest)
     }
-  }
-  most = row_max_u<LANES>(most);
-  if (!mine) return;
-  const int e = (int)(most >> 23);
-  // 448 = 1.75 2^8: a mantissa beyond 1.75 takes the next exponent
-  int s = FMT == 8 ? e - 8 + ((most & 0x7fffffu) > 0x600000u) : e - 14;
-  s = most == 0 ? kExpZero : max(s, 1);
-  const bool nan = e == 255;
-  if (nan) s = kExpNaN;
-  const float inv = nan ? 0.f : __uint_as_float((uint32_t)(254 - s) << 23);
+    most = row_max_u<LANES>(mine ? most : 0);
+    if (row[u] < 0) continue;
+    const int e = (int)(most >> 23);
+    // 448 = 1.75 2^8: a mantissa beyond 1.75 takes the next exponent
+    int s = FMT == 8 ? e - 8 + ((most & 0x7fffffu) > 0x600000u) : e - 14;
+    s = most == 0 ? kExpZero : max(s, 1);
+    const bool nan = e == 255;
+    if (nan) s = kExpNaN;
+    const float inv = nan ? 0.f : __uint_as_float((uint32_t)(254 - s) << 23);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = nan ? 0.f : x[j] * inv;
-  char *base = which ? a.c.v : a.c.k;
-  if constexpr (FMT == 8) {
-    const uintx2_t w = {pack_e4m3(x[0], x[1], x[2], x[3]), pack_e4m3(x[4], x[5], x[6], x[7])};
-    *reinterpret_cast<uintx2_t *>(base + row * dim + l * 8) = w;
-  } else {
-    const uintx4_t w = {pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7])};
-    *reinterpret_cast<uintx4_t *>(base + (row * dim + l * 8) * 2) = w;
+    for (int j = 0; j < 8; ++j) x[j] = nan ? 0.f : x[j] * inv;
+    char *base = which ? a.c.v : a.c.k;
+    if constexpr (FMT == 8) {
+      const uintx2_t w = {pack_e4m3(x[0], x[1], x[2], x[3]), pack_e4m3(x[4], x[5], x[6], x[7])};
+      *reinterpret_cast<uintx2_t *>(base + row[u] * dim + l * 8) = w;
+    } else {
+      const uintx4_t w = {pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7])};
+      *reinterpret_cast<uintx4_t *>(base + (row[u] * dim + l * 8) * 2) = w;
+    }
+    if (l == 0) (which ? a.c.v_exp : a.c.k_exp)[row[u]] = (uint8_t)s;
   }
-  if (l == 0) (which ? a.c.v_exp : a.c.k_exp)[row] = (uint8_t)s;
 }
 
 __device__ __forceinline__ float row_scale(int e) { return e == kExpNaN ? NAN : e == 0 ? 0x1p-127f : __uint_as_float((uint32_t)e << 23); }
@@ -118,41 +142,50 @@ __device__ __forceinline__ void put8(uint16_t *p, const float (&x)[8]) {
   __builtin_memcpy(p, w, 16);
 }
 
-template <typename TT, int FMT, int LANES>
+template <typename TT, int FMT, int LANES, int U>
 __global__ __launch_bounds__(256) void k_cache_read(RowsArgs a) {
   typedef typename TT::T T;
   constexpr int ROWS = 256 / LANES;
-  const int which = blockIdx.y, l = threadIdx.x % LANES;
-  const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  const int heads = a.c.heads, dim = a.c.dim;
-  const int h = (int)(r % heads);
-  const int64_t bn = r / heads;
-  const int n = (int)(bn % a.n), b = (int)(bn / a.n);
-  if (b >= a.B || l * 8 >= dim) return;
-  int64_t row = -1;
-  if (!(a.count && n >= a.count[b])) row = cache_row(a.c, b, (int64_t)a.start[b] + n, h);
-  float x[8] = {};
-  if (row >= 0) {
-    const float scale = row_scale((which ? a.c.v_exp : a.c.k_exp)[row]);
-    const char *base = which ? a.c.v : a.c.k;
-    uint32_t w[4];
-    if constexpr (FMT == 8) {
-      const uintx2_t q = *reinterpret_cast<const uintx2_t *>(base + row * dim + l * 8);
+  const int which = blockIdx.y, l = threadIdx.x % LANES, b = blockIdx.x / a.blocks, dim = a.c.dim;
+  const int r0 = (blockIdx.x - b * a.blocks) * ROWS * U + threadIdx.x / LANES;
+  const int start = a.start[b], count = a.count ? a.count[b] : a.n;
+  const char *base = which ? a.c.v : a.c.k;
+  const uint8_t *exps = which ? a.c.v_exp : a.c.k_exp;
+  int64_t row[U];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)q[j], 1.f, false));
-        w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)q[j], 1.f, true));
-      }
-    } else {
-      const uintx4_t q = *reinterpret_cast<const uintx4_t *>(base + (row * dim + l * 8) * 2);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = q[j];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)__builtin_bit_cast(f16x2_t, w[j / 2])[j % 2] * scale;
+  for (int u = 0; u < U; ++u) {
+    const RowAt at = row_at<LANES>(a, r0 + u * ROWS);
+    row[u] = at.mine && at.i < count ? cache_row(a.c, b, (int64_t)start + at.i, at.h) : -1;
   }
-  T *p = static_cast<T *>(a.out[which]) + b * a.stride_b[which] + n * a.stride_n[which] + h * a.stride_h[which] + l * 8;
-  put8(p, x);
+  uint32_t w[U][FMT / 4];
+  int e[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {  // (row 0 for rows that are not there)
+    const int64_t from = row[u] < 0 ? 0 : row[u] * dim + l * 8;
+    __builtin_memcpy(w[u], __builtin_assume_aligned(base + from * (FMT / 8), FMT), FMT);
+    e[u] = exps[row[u] < 0 ? 0 : row[u]];
+  }
+  T *out = static_cast<T *>(a.out[which]) + b * a.stride_b[which] + l * 8;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const RowAt at = row_at<LANES>(a, r0 + u * ROWS);
+    if (!at.mine) continue;
+    const float scale = row_scale(e[u]);
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t pair;
+      if constexpr (FMT == 8)
+        pair = __builtin_bit_cast(uint32_t, j % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[u][j / 2], 1.f, true)
+                                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[u][j / 2], 1.f, false));
+      else
+        pair = w[u][j];
+      const f16x2_t y = __builtin_bit_cast(f16x2_t, pair);
+      x[2 * j] = row[u] < 0 ? 0.f : (float)y[0] * scale;
+      x[2 * j + 1] = row[u] < 0 ? 0.f : (float)y[1] * scale;
+    }
+    put8(out + at.i * a.stride_n[which] + at.h * a.stride_h[which], x);
+  }
 }
 
 }  // namespace rb

@@ -25,7 +25,6 @@ __device__ __forceinline__ double exp2_d(double t) {
   return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
-constexpr int kSelTile = 32;   // logits a lane holds at a time
 constexpr int kSelBuf = 64;    // candidates that a wave ranks at a time: one per lane
 constexpr int kSelLists = 64;  // lists that a wave joins: one per lane
 
@@ -224,86 +223,101 @@ struct SelectArgs {
 };
 
 struct SelJoin {
-  SelList list[kSelLists];
-  SelStat stat[kSelLists];
-  double lse[kMaxBeam], score[kMaxBeam], cand_key[kSelLists * kMaxBeam];
+  double cand_key[kSelLists * kMaxBeam];
   int cand_at[kSelLists * kMaxBeam];
+  double sum[kSelLists];
+  float ref[kSelLists];
   int n;
 };
 
-// One wave: the `beam` best of an utterance from the lists of its rows (sh.list[k * parts + p]).  A bound that they reach is the beam-th largest of
-// the lists' first candidates; each lane hands on those of its list that reach it, and they are ranked by (key descending, flat index
-// ascending).
-__device__ __forceinline__ void join_lists(const SelectArgs &a, int b, SelJoin &sh) {
+// One wave: the `beam` best of an utterance from the lists of its rows, lane l's being list l = k * parts + p.  A bound that they reach is the
+// beam-th largest of the lists' first candidates; each lane hands on those of its list that reach it, and they are ranked by (key descending,
+// flat index ascending).
+__device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const SelList *lists, const SelStat *stats, SelJoin &sh) {
   const int lane = threadIdx.x & 63, beam = a.beam, parts = a.parts, n_lists = beam * parts;
-  const int k = lane / parts;
-  const bool have = lane < n_lists;
-  if (lane == 0) sh.n = 0;
-  // log sum exp of every row
-  SelStat st = have ? sh.stat[lane] : SelStat{0., -INFINITY, 0};
-  float ref = -INFINITY;
-  if (have)
-    for (int p = 0; p < parts; ++p) ref = fmaxf(ref, sh.stat[k * parts + p].ref);
-  // (a part that held nothing but -inf, or NaN: its sum is 0, or NaN, whatever it is multiplied by)
-  st.sum *= st.ref > -INFINITY ? exp((double)st.ref - ref) : 1.;
-  wave_lds_order();
-  if (have) sh.stat[lane].sum = st.sum;
-  wave_lds_order();
-  bool finished = false;
-  if (lane < beam) {
-    double s = 0.;
-    for (int p = 0; p < parts; ++p) s += sh.stat[lane * parts + p].sum;
-    float r = -INFINITY;
-    for (int p = 0; p < parts; ++p) r = fmaxf(r, sh.stat[lane * parts + p].ref);
-    sh.score[lane] = a.scores[(int64_t)b * beam + lane];
-    finished = a.done && a.done[(int64_t)b * beam + lane];
-    sh.lse[lane] = finished ? 0. : (double)r + log(s);
-    if (finished)  // its one candidate: eos, with the score that it has
-      for (int p = 0; p < parts; ++p) {
-        sh.list[lane * parts + p].v[0] = p == 0 ? 0.f : -INFINITY;
-        sh.list[lane * parts + p].i[0] = a.eos;
-        sh.list[lane * parts + p].v[1] = -INFINITY;
-      }
+  const int l = min(lane, n_lists - 1), k = l / parts;
+  // everything that is read leaves at once (what a finished hypothesis' lists hold is not looked at)
+  SelStat st = stats[l];
+  float v[kMaxBeam];
+  int i[kMaxBeam];
+  __builtin_memcpy(v, lists[l].v, sizeof(v));
+  __builtin_memcpy(i, lists[l].i, sizeof(i));
+  const double score = a.scores[(int64_t)b * beam + k];
+  const bool finished = a.done && a.done[(int64_t)b * beam + k];
+  const bool have = lane < n_lists && !(finished && lane != k * parts);
+  // log sum exp of the row
+  float ref = st.ref;
+  double sum = st.sum;
+  if (parts > 1) {
+    sh.ref[lane] = ref;
+    wave_lds_order();
+    for (int p = 0; p < parts; ++p) ref = fmaxf(ref, sh.ref[k * parts + p]);
+    // (a part that held nothing but -inf, or NaN: its sum is 0, or NaN, whatever it is multiplied by)
+    sh.sum[lane] = st.ref > -INFINITY ? sum * exp((double)st.ref - ref) : sum;
+    wave_lds_order();
+    sum = 0.;
+    for (int p = 0; p < parts; ++p) sum += sh.sum[k * parts + p];
   }
-  wave_lds_order();
-  const double score = have ? sh.score[k] : 0., lse = have ? sh.lse[k] : 0.;
-  auto key_of = [&](float v) {
-    const double key = score + ((double)v - lse);
-    return key == key && v > -INFINITY ? key : (double)-INFINITY;
+  const double lse = (double)ref + log(sum);
+  auto key_of = [&](float x) {
+    const double key = score + ((double)x - lse);
+    return key == key && x > -INFINITY ? key : (double)-INFINITY;
   };
-  const double head = have ? key_of(sh.list[lane].v[0]) : -INFINITY;
+  double head = have ? key_of(v[0]) : -INFINITY;
+  if (finished) {  // its one candidate: eos, with the score that it has
+    head = have && score == score ? score : -INFINITY;
+    i[0] = a.eos;
+  }
+  if (lane == 0) sh.n = 0;
   int rank = 0;
+#pragma unroll 4
   for (int j = 0; j < n_lists; ++j) rank += comes_before_count(readlane_d(head, j), j, head, lane);
-  const uint64_t at = __ballot(have && rank == beam - 1);
+  const uint64_t at = __ballot(lane < n_lists && rank == beam - 1);
   const double bound = readlane_d(head, __ffsll((unsigned long long)at) - 1);
-  int mine = 0;
-  if (have && head > -INFINITY)
-    while (mine < beam) {
-      const double key = key_of(sh.list[lane].v[mine]);
-      if (!(key >= bound && key > -INFINITY)) break;
-      ++mine;
+  wave_lds_order();
+  if (have && head > -INFINITY && head >= bound) {
+    double key[kMaxBeam] = {head};
+    int mine = 1;
+    bool more = !finished;
+#pragma unroll
+    for (int j = 1; j < kMaxBeam; ++j) {
+      key[j] = key_of(v[j]);
+      more = more && j < beam && key[j] > -INFINITY && key[j] >= bound;
+      mine += more;
     }
-  if (mine) {
     const int pos = atomicAdd(&sh.n, mine);
-    for (int j = 0; j < mine; ++j) {
-      sh.cand_key[pos + j] = key_of(sh.list[lane].v[j]);
-      sh.cand_at[pos + j] = k * a.V + sh.list[lane].i[j];
-    }
+#pragma unroll
+    for (int j = 0; j < kMaxBeam; ++j)
+      if (j < mine) {
+        sh.cand_key[pos + j] = key[j];
+        sh.cand_at[pos + j] = k * a.V + i[j];
+      }
   }
   wave_lds_order();
   const int n = sh.n;
   const int64_t out = (int64_t)b * beam;
-  for (int c = lane; c < n; c += 64) {
-    const double key = sh.cand_key[c];
-    const int flat = sh.cand_at[c];
+  auto put = [&](int r, double key, int flat) {
+    const int parent = flat / a.V, token = flat - parent * a.V;
+    a.out_scores[out + r] = key;
+    a.out_parent[out + r] = parent;
+    a.out_token[out + r] = token;
+    if (a.out_done) a.out_done[out + r] = token == a.eos;
+  };
+  if (n <= 64) {
+    const double key = lane < n ? sh.cand_key[lane] : -INFINITY;
+    const int flat = lane < n ? sh.cand_at[lane] : 0x7fffffff;
     int r = 0;
-    for (int j = 0; j < n; ++j) r += comes_before_count(sh.cand_key[j], sh.cand_at[j], key, flat);
-    if (r < beam) {
-      const int parent = flat / a.V, token = flat - parent * a.V;
-      a.out_scores[out + r] = key;
-      a.out_parent[out + r] = parent;
-      a.out_token[out + r] = token;
-      if (a.out_done) a.out_done[out + r] = token == a.eos;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) r += comes_before_count(readlane_d(key, j), __builtin_amdgcn_readlane(flat, j), key, flat);
+    if (lane < n && r < beam) put(r, key, flat);
+  } else {
+    for (int c = lane; c < n; c += 64) {
+      const double key = sh.cand_key[c];
+      const int flat = sh.cand_at[c];
+      int r = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) r += comes_before_count(sh.cand_key[j], sh.cand_at[j], key, flat);
+      if (r < beam) put(r, key, flat);
     }
   }
   for (int r = n + lane; r < beam; r += 64) {  // empty slots
@@ -324,10 +338,12 @@ __device__ __forceinline__ void put_list(const RowPart &part, double sum, bool b
 }
 
 // ---- everything of an utterance in one block of 16 waves, parts = 16 / beam of them for a row: no workspace, one launch
-template <typename TT>
+template <typename TT, int NV>
 __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
   typedef typename TT::T T;
   __shared__ SelJoin sh;
+  __shared__ SelList list[16];
+  __shared__ SelStat stat[16];
   __shared__ CandBuf buf[16];
   const int b = blockIdx.x, wave = threadIdx.x >> 6, k = wave / a.parts, p = wave - k * a.parts;
   if (k < a.beam) {
@@ -335,64 +351,167 @@ __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
     if (!(a.done && a.done[(int64_t)b * a.beam + k])) {
       const T *row = static_cast<const T *>(a.logits) + b * a.stride_b + k * a.stride_k;
       const int begin = min(p * a.part_len, a.V);
-      scan_row<T, 16>(row, begin, min(begin + a.part_len, a.V), a.beam, part, buf[wave]);
+      scan_row<T, NV * 16 / sizeof(T)>(row, begin, min(begin + a.part_len, a.V), a.beam, part, buf[wave]);
     }
     const double sum = wave_sum_d(part.sum);
-    put_list(part, sum, __any(part.bad), a.beam, sh.list[wave], sh.stat[wave]);
+    put_list(part, sum, __any(part.bad), a.beam, list[wave], stat[wave]);
   }
   __syncthreads();
-  if (wave == 0) join_lists(a, b, sh);
+  if (wave == 0) join_lists(a, b, list, stat, sh);
 }
 
-// ---- many blocks for a row: each leaves the best of its part, a second launch joins them
-template <typename TT>
+// ---- many blocks for a row: each leaves the best of its part, a second launch joins them.  A block's four waves take tiles of 256 E logits
+// together: a bound that the `beam` best of a tile reach is the beam-th largest of the maxima of 32 groups of 8 lanes; of the logits
+// that reach it and what earlier tiles left, rarely more than twice `beam`, one wave takes the best.
+struct SelScan {
+  float group[32];
+  CandBuf buf;  // the list, in its first `beam` places, and what a tile adds
+  int n;
+  CandBuf wave_buf[4];
+  SelList list[4];
+  SelStat stat[4];
+};
+
+template <typename TT, int E>
 __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
   typedef typename TT::T T;
-  __shared__ CandBuf buf[4];
-  __shared__ SelList list[4];
-  __shared__ SelStat stat[4];
-  const int p = blockIdx.x % a.parts, row_i = blockIdx.x / a.parts, b = row_i / a.beam, k = row_i - b * a.beam;
+  constexpr int VE = 16 / sizeof(T), NV = E / VE, FOURS = E / 4;
+  __shared__ SelScan sh;
+  const int p = blockIdx.x % a.parts, row_i = blockIdx.x / a.parts, b = row_i / a.beam, k = row_i - b * a.beam, beam = a.beam;
   if (a.done && a.done[row_i]) return;  // (the join takes nothing from its lists)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const T *row = static_cast<const T *>(a.logits) + b * a.stride_b + k * a.stride_k;
-  const int len = a.part_len >> 2, begin = min(p * a.part_len + wave * len, a.V);
-  RowPart part;
-  scan_row<T, kSelTile>(row, begin, min(begin + len, a.V), a.beam, part, buf[wave]);
-  const double sum = wave_sum_d(part.sum);
-  put_list(part, sum, __any(part.bad), a.beam, list[wave], stat[wave]);
+  const int begin = min(p * a.part_len, a.V), end = min(begin + a.part_len, a.V);
+  const int64_t at = (int64_t)row_i * a.parts + p;
+  double sum = 0.;
+  float ref = -INFINITY, last = -INFINITY;  // of the block's list: its beam-th
+  bool bad = false, many = false;
+  if (threadIdx.x < kSelBuf) {
+    sh.buf.v[threadIdx.x] = -INFINITY;
+    sh.buf.i[threadIdx.x] = 0x7fffffff;
+  }
+  for (int base = begin; base < end; base += 256 * E) {
+    float x[E];
+    const int mine = base + wave * 64 * E + lane * VE;  // of vector i: 64 VE i further on
+    if (base + 256 * E <= end) {
+      T raw[NV][VE];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load16(row + mine + i * 64 * VE, raw[i]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) x[i * VE + j] = to_float(raw[i][j]);
+    } else {
+      // vectors that end behind the row read its last 16 bytes (a row here is longer), shifted
+      T raw[NV][VE];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load16(row + min(mine + i * 64 * VE, a.V - VE), raw[i]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int first = mine + i * 64 * VE, off = first - min(first, a.V - VE);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          float v = -INFINITY;
+#pragma unroll
+          for (int u = j; u < VE; ++u) v = j + off == u ? to_float(raw[i][u]) : v;
+          x[i * VE + j] = first + j < end ? v : -INFINITY;
+        }
+      }
+    }
+    float four[FOURS];  // NaN if one of them is
+#pragma unroll
+    for (int e = 0; e < FOURS; ++e)
+      four[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[4 * e], x[4 * e + 1]), __builtin_elementwise_maximum(x[4 * e + 2], x[4 * e + 3]));
+    float top = four[0];
+#pragma unroll
+    for (int e = 1; e < FOURS; ++e) top = __builtin_elementwise_maximum(top, four[e]);
+    bad |= !(top < INFINITY);
+    const float eight = group_max<8>(top);
+    if ((lane & 7) == 0) sh.group[wave * 8 + (lane >> 3)] = eight;
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    const float g = sh.group[lane & 31];
+    const float most = wave_max(g);
+    if (most > -INFINITY) {
+      if (!(most < ref + 500.f)) {  // (the first tile too; float64 holds exp(500) times exp(200) more)
+        const float to = most < INFINITY ? most : 0.f;
+        sum *= ref == -INFINITY ? 0. : exp((double)ref - to);
+        ref = to;
+      }
+      const double r = ref;
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum += exp2_d(((double)x[e] - r) * kLog2E);
+    }
+    // (equal logits come after those of the list, whose indices are smaller)
+    if (!many && most > last) {
+      // (the groups' maxima made different by their number in the last bits: a little smaller, which a bound may be)
+      const uint32_t key = (orderable(g) & ~31u) | (lane & 31);
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < 32; ++j) rank += (uint32_t)__builtin_amdgcn_readlane((int)key, j) > key;
+      const uint32_t nth = __builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(rank == beam - 1)) - 1) & ~31u;
+      const uint32_t after = orderable(last) + 1;
+      const float bound = from_orderable(nth > after ? nth : after);
+#pragma unroll
+      for (int f = 0; f < FOURS; ++f) {
+        if (!__any(four[f] >= bound)) continue;
+#pragma unroll
+        for (int e = 4 * f; e < 4 * f + 4; ++e)
+          if (x[e] >= bound) {
+            const int pos = beam + atomicAdd(&sh.n, 1);
+            if (pos < kSelBuf) {
+              sh.buf.v[pos] = x[e];
+              sh.buf.i[pos] = mine + (e / VE) * 64 * VE + e % VE;
+            }
+          }
+      }
+    }
+    __syncthreads();
+    const int n = sh.n;
+    if (n) {
+      many = many || beam + n > kSelBuf;
+      if (!many && wave == 0) {
+        const bool in = lane < beam + n;
+        float v = in ? sh.buf.v[lane] : -INFINITY;
+        int i = in ? sh.buf.i[lane] : 0x7fffffff;
+        rank_candidates(v, i, beam + n, beam, sh.buf, v, i);
+      }
+      __syncthreads();
+      last = sh.buf.v[beam - 1];
+    }
+  }
+  if (lane == 0) sh.stat[wave].sum = 0.;
+  sum = wave_sum_d(sum);
+  if (lane == 0) sh.stat[wave].sum = __any(bad) ? (double)NAN : sum;
+  if (many) {
+    // more candidates than a wave ranks at a time (many equal logits): each wave its own quarter's best, one after the other
+    RowPart part;
+    const int len = ((end - begin + 3) / 4 + VE - 1) / VE * VE, first = min(begin + wave * len, end);
+    scan_row<T, 8>(row, first, min(first + len, end), beam, part, sh.wave_buf[wave]);
+    put_list(part, 0., false, beam, sh.list[wave], sh.stat[wave]);
+    if (lane == 0) sh.stat[wave].sum = __any(bad) ? (double)NAN : sum;
+    __syncthreads();
+    if (wave == 0) {
+      const int w = lane / beam, e = lane - w * beam;
+      const bool in = lane < 4 * beam;
+      float v = in ? sh.list[w].v[e] : -INFINITY;
+      int i = in ? sh.list[w].i[e] : 0x7fffffff;
+      rank_candidates(v, i, 4 * beam, beam, sh.buf, v, i);
+    }
+  }
   __syncthreads();
   if (wave) return;
-  const int n = 4 * a.beam, w = lane / a.beam, e = lane - w * a.beam;  // at most 64
-  float v;
-  int i;
-  rank_candidates(lane < n ? list[w].v[e] : -INFINITY, lane < n ? list[w].i[e] : 0x7fffffff, n, a.beam, buf[0], v, i);
-  const int64_t at = (int64_t)row_i * a.parts + p;
-  if (lane < a.beam) {
-    a.lists[at].v[lane] = v;
-    a.lists[at].i[lane] = i;
+  if (lane < beam) {
+    a.lists[at].v[lane] = sh.buf.v[lane];
+    a.lists[at].i[lane] = sh.buf.i[lane];
   }
-  if (lane == 0) {
-    float ref = -INFINITY;
-    double s = 0.;
-    for (int j = 0; j < 4; ++j) ref = fmaxf(ref, stat[j].ref);
-    for (int j = 0; j < 4; ++j) s += stat[j].sum * (stat[j].ref > -INFINITY ? exp((double)stat[j].ref - ref) : 1.);
-    a.stats[at] = SelStat{s, ref, 0};
-  }
+  if (lane == 0) a.stats[at] = SelStat{(sh.stat[0].sum + sh.stat[1].sum) + (sh.stat[2].sum + sh.stat[3].sum), ref, 0};
 }
 
-static __global__ __launch_bounds__(256) void k_select_join(SelectArgs a) {
+static __global__ __launch_bounds__(64) void k_select_join(SelectArgs a) {
   __shared__ SelJoin sh;
-  const int b = blockIdx.x, n = a.beam * a.parts;
-  const int64_t first = (int64_t)b * n;
-  for (int e = threadIdx.x; e < n * kMaxBeam; e += 256) {
-    const int l = e / kMaxBeam, j = e % kMaxBeam;
-    const bool there = j < a.beam && !(a.done && a.done[(int64_t)b * a.beam + l / a.parts]);
-    sh.list[l].v[j] = there ? a.lists[first + l].v[j] : -INFINITY;
-    sh.list[l].i[j] = there ? a.lists[first + l].i[j] : 0x7fffffff;
-    if (j == 0) sh.stat[l] = there ? a.stats[first + l] : SelStat{0., -INFINITY, 0};
-  }
-  __syncthreads();
-  if (threadIdx.x < 64) join_lists(a, b, sh);
+  const int64_t first = (int64_t)blockIdx.x * a.beam * a.parts;
+  join_lists(a, blockIdx.x, a.lists + first, a.stats + first, sh);
 }
 
 // ---- states of hypotheses to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]]
@@ -423,17 +542,17 @@ __global__ __launch_bounds__(256) void k_reorder(ReorderArgs a) {
   const int inner = row % s.inner;
   row /= s.inner;
   const int b = row % a.B, lead = row / a.B;
-  int parent[BEAM];
+  int parent[BEAM];  // the same for all lanes: branches, not masks
 #pragma unroll
   for (int k = 0; k < BEAM; ++k) {
-    const int p = k < a.beam ? a.parent[(int64_t)b * a.beam + k] : k;
+    const int p = k < a.beam ? __builtin_amdgcn_readfirstlane(a.parent[(int64_t)b * a.beam + k]) : k;
     parent[k] = p >= 0 && p < a.beam ? p : k;  // an empty slot keeps what it holds
   }
   const int64_t at = ((int64_t)chunk * 256 + threadIdx.x) * sizeof(V);
   if (at >= s.row_bytes) return;
-  char *p = s.data + lead * s.lead_stride + b * s.b_stride + inner * s.inner_stride + at;
+  char *const p = s.data + lead * s.lead_stride + b * s.b_stride + inner * s.inner_stride + at;
   const int64_t slot_stride = s.slot_stride;
-  V v[BEAM];
+  V v[BEAM] = {};
 #pragma unroll
   for (int k = 0; k < BEAM; ++k)
     if (parent[k] != k) v[k] = *reinterpret_cast<const V *>(p + parent[k] * slot_stride);
