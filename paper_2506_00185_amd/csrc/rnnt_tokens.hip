@@ -51,13 +51,6 @@ int select_typed(const SelectArgs &a, bool one, hipStream_t stream) {
   return rc ? rc : launch(k_select_join, a.B, 1, 64, a, stream);
 }
 
-template <typename V>
-int reorder_width(const ReorderArgs &a, int blocks, hipStream_t stream) {
-  if (a.beam <= 4) return launch(k_reorder<V, 4>, blocks, 1, 256, a, stream);
-  if (a.beam <= 8) return launch(k_reorder<V, 8>, blocks, 1, 256, a, stream);
-  return launch(k_reorder<V, 16>, blocks, 1, 256, a, stream);
-}
-
 int64_t select_lists(int B, int beam, const SelectPlan &p) { return p.one ? 0 : (int64_t)B * beam * p.parts; }
 
 }  // namespace
@@ -118,8 +111,12 @@ int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rn
   if (B < 1) return refuse("B must be at least 1");
   if (beam < 1 || beam > kMaxBeam) return refuse("beam must be 1 to 16");
   if (n < 0 || n > kMaxStates) return refuse("at most 16 tensors");
-  StateView view[kMaxStates];
-  int vec[kMaxStates], used = 0;  // bytes of one access to each
+  ReorderArgs a;
+  a.parent = parent;
+  a.B = B;
+  a.beam = beam;
+  a.n = 0;
+  int64_t blocks = 0;
   for (int t = 0; t < n; ++t) {
     const rnnt_states_t &s = states[t];
     if (s.lead < 0 || s.inner < 0 || s.row_bytes < 0) return refuse("negative size");
@@ -141,7 +138,7 @@ int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rn
     }
     for (int u = 0; u < t; ++u)
       if (states[u].data == s.data && states[u].lead && states[u].inner && states[u].row_bytes) return refuse("a tensor is named twice");
-    StateView &v = view[used];
+    StateView &v = a.s[a.n++];
     v.data = static_cast<char *>(s.data);
     v.lead_stride = s.lead_stride;
     v.b_stride = s.b_stride;
@@ -150,49 +147,24 @@ int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rn
     v.row_bytes = s.row_bytes;
     v.lead = s.lead;
     v.inner = s.inner;
-    const uint64_t all = (uint64_t)(uintptr_t)s.data | (uint64_t)s.row_bytes | (s.lead > 1 ? (uint64_t)s.lead_stride : 0) | (B > 1 ? (uint64_t)s.b_stride : 0) |
-                         (beam > 1 ? (uint64_t)s.slot_stride : 0) | (s.inner > 1 ? (uint64_t)s.inner_stride : 0);
-    int w = 16;
-    while (all % w) w >>= 1;
-    vec[used++] = w;
-    const int64_t chunks = (s.row_bytes / w + 255) / 256;
+    const int64_t chunks = ((s.row_bytes >> 4) + (s.row_bytes & 15) + 255) / 256;
     // (each factor is below 2^31, and a product beyond what a launch takes is refused before the next one is formed)
     int64_t count = chunks;
     if (count > 0x7fffffff) return refuse("more work than one launch takes");
     for (int64_t f : {(int64_t)s.lead, (int64_t)B, (int64_t)s.inner}) {
       count *= f;
-      if (count > 0x7fffffff / kMaxStates) return refuse("more work than one launch takes");
+      if (count > 0x7fffffff) return refuse("more work than one launch takes");
     }
     v.chunks = (int)chunks;
+    v.first_block = (int)blocks;
+    blocks += count;
+    if (blocks > 0x7fffffff) return refuse("more work than one launch takes");
   }
-  if (beam == 1) return RNNT_OK;
+  if (!a.n || beam == 1) return RNNT_OK;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  for (int w = 16; w; w >>= 1) {  // one launch for all tensors of a width, which are one or two widths as a rule
-    ReorderArgs a;
-    a.parent = parent;
-    a.B = B;
-    a.beam = beam;
-    a.n = 0;
-    int blocks = 0;
-    for (int t = 0; t < used; ++t) {
-      if (vec[t] != w) continue;
-      StateView &v = a.s[a.n++];
-      v = view[t];
-      v.first_block = blocks;
-      blocks += v.chunks * v.lead * B * v.inner;
-    }
-    if (!a.n) continue;
-    int rc = 0;
-    switch (w) {
-      case 16: rc = reorder_width<uintx4_t>(a, blocks, stream); break;
-      case 8: rc = reorder_width<uintx2_t>(a, blocks, stream); break;
-      case 4: rc = reorder_width<uint32_t>(a, blocks, stream); break;
-      case 2: rc = reorder_width<uint16_t>(a, blocks, stream); break;
-      case 1: rc = reorder_width<uint8_t>(a, blocks, stream); break;
-    }
-    if (rc) return rc;
-  }
-  return RNNT_OK;
+  if (beam <= 4) return launch(k_reorder<4>, blocks, 1, 256, a, stream);
+  if (beam <= 8) return launch(k_reorder<8>, blocks, 1, 256, a, stream);
+  return launch(k_reorder<16>, blocks, 1, 256, a, stream);
 } catch (const std::bad_alloc &) {
   return RNNT_E_NOMEM;
 } catch (...) {

@@ -223,6 +223,7 @@ struct SelectArgs {
 };
 
 struct SelJoin {
+  double key[kSelLists][kMaxBeam + 1];  // of the lists' candidates
   double cand_key[kSelLists * kMaxBeam];
   int cand_at[kSelLists * kMaxBeam];
   double sum[kSelLists];
@@ -231,20 +232,19 @@ struct SelJoin {
 };
 
 // One wave: the `beam` best of an utterance from the lists of its rows, lane l's being list l = k * parts + p.  A bound that they reach is the
-// beam-th largest of the lists' first candidates; each lane hands on those of its list that reach it, and they are ranked by (key descending,
-// flat index ascending).
+// beam-th largest of the first few of every list; each lane hands on those of its list that reach it, and they are
+// ranked by (key descending, flat index ascending).
 __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const SelList *lists, const SelStat *stats, SelJoin &sh) {
   const int lane = threadIdx.x & 63, beam = a.beam, parts = a.parts, n_lists = beam * parts;
   const int l = min(lane, n_lists - 1), k = l / parts;
   // everything that is read leaves at once (what a finished hypothesis' lists hold is not looked at)
-  SelStat st = stats[l];
+  const SelStat st = stats[l];
   float v[kMaxBeam];
   int i[kMaxBeam];
   __builtin_memcpy(v, lists[l].v, sizeof(v));
   __builtin_memcpy(i, lists[l].i, sizeof(i));
   const double score = a.scores[(int64_t)b * beam + k];
   const bool finished = a.done && a.done[(int64_t)b * beam + k];
-  const bool have = lane < n_lists && !(finished && lane != k * parts);
   // log sum exp of the row
   float ref = st.ref;
   double sum = st.sum;
@@ -259,32 +259,32 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     for (int p = 0; p < parts; ++p) sum += sh.sum[k * parts + p];
   }
   const double lse = (double)ref + log(sum);
-  auto key_of = [&](float x) {
-    const double key = score + ((double)x - lse);
-    return key == key && x > -INFINITY ? key : (double)-INFINITY;
-  };
-  double head = have ? key_of(v[0]) : -INFINITY;
-  if (finished) {  // its one candidate: eos, with the score that it has
-    head = have && score == score ? score : -INFINITY;
+  double key[kMaxBeam];
+#pragma unroll
+  for (int j = 0; j < kMaxBeam; ++j) {
+    key[j] = score + ((double)v[j] - lse);
+    if (!(key[j] == key[j] && v[j] > -INFINITY && j < beam) || finished || lane >= n_lists) key[j] = -INFINITY;
+  }
+  if (finished && lane == k * parts) {  // its one candidate: eos, with the score that it has
+    key[0] = score == score ? score : -INFINITY;
     i[0] = a.eos;
   }
-  if (lane == 0) sh.n = 0;
-  int rank = 0;
-#pragma unroll 4
-  for (int j = 0; j < n_lists; ++j) rank += comes_before_count(readlane_d(head, j), j, head, lane);
-  const uint64_t at = __ballot(lane < n_lists && rank == beam - 1);
-  const double bound = readlane_d(head, __ffsll((unsigned long long)at) - 1);
-  wave_lds_order();
-  if (have && head > -INFINITY && head >= bound) {
-    double key[kMaxBeam] = {head};
-    int mine = 1;
-    bool more = !finished;
 #pragma unroll
-    for (int j = 1; j < kMaxBeam; ++j) {
-      key[j] = key_of(v[j]);
-      more = more && j < beam && key[j] > -INFINITY && key[j] >= bound;
-      mine += more;
-    }
+  for (int j = 0; j < kMaxBeam; ++j) sh.key[lane][j] = key[j];
+  if (lane == 0) sh.n = 0;
+  wave_lds_order();
+  // the bound, in float32 rounded down
+  const int firsts = max(min(64, 4 * beam) / n_lists, 1), list = lane / firsts;
+  const double one = list < n_lists ? sh.key[list][lane - list * firsts] : -INFINITY;
+  const float low = one > -INFINITY ? from_orderable(orderable((float)one) - 1) : -INFINITY;
+  int before = 0;
+#pragma unroll 8
+  for (int j = 0; j < n_lists * firsts; ++j) before += readlane_f(low, j) > low;
+  const float bound = -wave_max(before < beam ? -low : -INFINITY);
+  int mine = 0;
+#pragma unroll
+  for (int j = 0; j < kMaxBeam; ++j) mine += key[j] > -INFINITY && key[j] >= (double)bound;  // (a list's keys descend)
+  if (mine) {
     const int pos = atomicAdd(&sh.n, mine);
 #pragma unroll
     for (int j = 0; j < kMaxBeam; ++j)
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
   for (int base = begin; base < end; base += 256 * E) {
     float x[E];
     const int mine = base + wave * 64 * E + lane * VE;  // of vector i: 64 VE i further on
-    if (base + 256 * E <= end) {
+    if (base + (wave + 1) * 64 * E <= end) {
       T raw[NV][VE];
 #pragma unroll
       for (int i = 0; i < NV; ++i) load16(row + mine + i * 64 * VE, raw[i]);
@@ -531,8 +531,20 @@ struct ReorderArgs {
   StateView s[kMaxStates];
 };
 
-// V: the widest access that every address and length of the launch's tensors allows
+typedef uintx4_t uintx4_any __attribute__((aligned(1)));  // at any address
+
 template <typename V, int BEAM>
+__device__ __forceinline__ void move_column(char *p, int64_t slot_stride, const int (&parent)[BEAM], int beam) {
+  V v[BEAM];  // (of a slot that stays, itself: without branches all loads leave at once)
+#pragma unroll
+  for (int k = 0; k < BEAM; ++k) v[k] = *reinterpret_cast<const V *>(p + (k < beam ? parent[k] : 0) * slot_stride);
+#pragma unroll
+  for (int k = 0; k < BEAM; ++k)
+    if (parent[k] != k) *reinterpret_cast<V *>(p + k * slot_stride) = v[k];
+}
+
+// A column is 16 bytes from any address; what a row has behind its last 16 is columns of one byte
+template <int BEAM>
 __global__ __launch_bounds__(256) void k_reorder(ReorderArgs a) {
   int t = 0;
   while (t + 1 < a.n && (int)blockIdx.x >= a.s[t + 1].first_block) ++t;
@@ -548,17 +560,10 @@ __global__ __launch_bounds__(256) void k_reorder(ReorderArgs a) {
     const int p = k < a.beam ? __builtin_amdgcn_readfirstlane(a.parent[(int64_t)b * a.beam + k]) : k;
     parent[k] = p >= 0 && p < a.beam ? p : k;  // an empty slot keeps what it holds
   }
-  const int64_t at = ((int64_t)chunk * 256 + threadIdx.x) * sizeof(V);
-  if (at >= s.row_bytes) return;
-  char *const p = s.data + lead * s.lead_stride + b * s.b_stride + inner * s.inner_stride + at;
-  const int64_t slot_stride = s.slot_stride;
-  V v[BEAM] = {};
-#pragma unroll
-  for (int k = 0; k < BEAM; ++k)
-    if (parent[k] != k) v[k] = *reinterpret_cast<const V *>(p + parent[k] * slot_stride);
-#pragma unroll
-  for (int k = 0; k < BEAM; ++k)
-    if (parent[k] != k) *reinterpret_cast<V *>(p + k * slot_stride) = v[k];
+  const int64_t column = (int64_t)chunk * 256 + threadIdx.x, wide = s.row_bytes >> 4;
+  char *const p = s.data + lead * s.lead_stride + b * s.b_stride + inner * s.inner_stride;
+  if (column < wide) move_column<uintx4_any, BEAM>(p + column * 16, s.slot_stride, parent, a.beam);
+  else if (column - wide < (s.row_bytes & 15)) move_column<uint8_t, BEAM>(p + wide * 16 + (column - wide), s.slot_stride, parent, a.beam);
 }
 
 }  // namespace rb
