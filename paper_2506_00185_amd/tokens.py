@@ -48,58 +48,64 @@ def _refuse(ok, what):
         raise RnntBeamError(what)
 
 
-def _types():
-    import torch
-    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+class _Torch:
+    """What the calls below need of torch, looked up once: a call is a few microseconds in all."""
+
+    def __init__(self):
+        import torch
+        self.empty, self.empty_like, self.device_of = torch.empty, torch.empty_like, torch.cuda.current_device
+        self.f64, self.f32, self.i32, self.u8, self.bool = torch.float64, torch.float32, torch.int32, torch.uint8, torch.bool
+        self.types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        # (the pointer alone where this torch gives it without an object around it)
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        self.lib = load_library()
 
 
-_TYPES = None
+_loaded = None
 
 
-def _type_of(t, what):
-    global _TYPES
-    if _TYPES is None:
-        _TYPES = _types()
-    code = _TYPES.get(t.dtype)
-    _refuse(code is not None, f"{what} must be float32, float16 or bfloat16")
+def _torch():
+    global _loaded
+    if _loaded is None:
+        _loaded = _Torch()
+    return _loaded
+
+
+def _type_of(T, t, what):
+    code = T.types.get(t.dtype)
+    if code is None:
+        raise RnntBeamError(f"{what} must be float32, float16 or bfloat16")
     return code
 
 
 def _array(t, what, dtype, shape, device):
     """Pointer of a contiguous tensor of that type, shape and device."""
-    _refuse(t.dtype == dtype, f"{what} must be {dtype}")
-    _refuse(t.device == device, f"{what} is on {t.device}, not on {device}")
-    _refuse(tuple(t.shape) == shape, f"{what} must have shape {shape}, not {tuple(t.shape)}")
-    _refuse(t.is_contiguous(), f"{what} must be contiguous")
+    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        _refuse(t.dtype == dtype, f"{what} must be {dtype}")
+        _refuse(t.device == device, f"{what} is on {t.device}, not on {device}")
+        _refuse(t.shape == shape, f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        raise RnntBeamError(f"{what} must be contiguous")
     return t.data_ptr()
 
 
-class _Call:
-    """Device and stream of a call: ``with _Call(tensor, stream, inputs) as raw`` gives the stream's pointer; allocations inside belong to it."""
-
-    def __init__(self, t, stream, inputs):
-        import torch
-        _refuse(t.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
-        self.stack = None
-        if torch.cuda.current_device() != t.device.index:
-            self.stack = contextlib.ExitStack()
-            self.stack.enter_context(torch.cuda.device(t.device))
-        current = torch.cuda.current_stream(t.device)
-        if stream is not None and stream != current:
-            _refuse(stream.device == t.device, f"the stream is of {stream.device}, the tensors are on {t.device}")
-            for x in inputs:  # of another stream: not to be given away before this call has used them
-                if x is not None:
-                    x.record_stream(stream)
-            self.stack = self.stack or contextlib.ExitStack()
-            self.stack.enter_context(torch.cuda.stream(stream))
-        self.raw = (stream or current).cuda_stream
-
-    def __enter__(self):
-        return C.c_void_p(self.raw)
-
-    def __exit__(self, *exc):
-        if self.stack is not None:
-            self.stack.close()
+def _enter(T, t, stream, inputs):
+    """(pointer of the stream, what to close behind the call): the call's device and stream are the current ones in between, so that what
+    it allocates belongs to them."""
+    if not t.is_cuda:
+        raise RnntBeamError("tensors must be on the GPU: there is no CPU fallback")
+    index = t.get_device()
+    if stream is None and index == T.device_of():
+        return C.c_void_p(T.raw_stream(index)), None
+    import torch
+    scope = contextlib.ExitStack()
+    scope.enter_context(torch.cuda.device(index))
+    if stream is not None and stream != torch.cuda.current_stream(index):
+        _refuse(stream.device == t.device, f"the stream is of {stream.device}, the tensors are on {t.device}")
+        for x in inputs:  # of another stream: not to be given away before this call has used them
+            if x is not None:
+                x.record_stream(stream)
+        scope.enter_context(torch.cuda.stream(stream))
+    return C.c_void_p((stream or torch.cuda.current_stream(index)).cuda_stream), scope
 
 
 def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
@@ -107,42 +113,48 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     the hypotheses' scores float64 [B, beam].  Returns (scores float64, parents int32, tokens int32, done bool or None), each [B, beam].
     ``eos``: the token that finishes a hypothesis (-1: none), ``done`` bool [B, beam]: which have finished.  ``out``: such a tuple to write
     to; it may hold ``scores`` and ``done`` themselves."""
-    import torch
-    _refuse(logits.dim() == 3, "logits must be [B, beam, V]")
+    T = _torch()
+    if logits.dim() != 3:
+        raise RnntBeamError("logits must be [B, beam, V]")
     B, beam, V = logits.shape
-    _refuse(V >= 1 and (V == 1 or logits.stride(2) == 1), "the last dimension of logits must be contiguous")
-    dev = logits.device
-    s = _Select(struct_size=C.sizeof(_Select), type=_type_of(logits, "logits"), B=B, beam=beam, V=V, eos=eos, logits=logits.data_ptr(),
-                stride_b=logits.stride(0), stride_k=logits.stride(1))
-    s.scores = _array(scores, "scores", torch.float64, (B, beam), dev)
+    stride_b, stride_k, stride_v = logits.stride()
+    if V < 1 or (V > 1 and stride_v != 1):
+        raise RnntBeamError("the last dimension of logits must be contiguous")
+    dev, shape = logits.device, (B, beam)
+    s = _Select(C.sizeof(_Select), _type_of(T, logits, "logits"), B, beam, V, eos, logits.data_ptr(), stride_b, stride_k,
+                _array(scores, "scores", T.f64, shape, dev))
     if done is not None:
-        s.done = _array(done, "done", torch.bool, (B, beam), dev)
-    lib = load_library()
-    with _Call(logits, stream, (logits, scores, done) + tuple(out or ())) as raw:
+        s.done = _array(done, "done", T.bool, shape, dev)
+    raw, scope = _enter(T, logits, stream, (logits, scores, done) + tuple(out or ()))
+    try:
         if out is None:
-            out = (torch.empty((B, beam), dtype=torch.float64, device=dev), torch.empty((B, beam), dtype=torch.int32, device=dev),
-                   torch.empty((B, beam), dtype=torch.int32, device=dev),
-                   torch.empty((B, beam), dtype=torch.bool, device=dev) if eos >= 0 else None)
-            s.out_scores, s.out_parent, s.out_token = (t.data_ptr() for t in out[:3])
+            out = (T.empty_like(scores), T.empty(shape, dtype=T.i32, device=dev), T.empty(shape, dtype=T.i32, device=dev),
+                   T.empty(shape, dtype=T.bool, device=dev) if eos >= 0 else None)
+            s.out_scores, s.out_parent, s.out_token = out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr()
         else:
             _refuse(len(out) == 4, "out must be (scores, parents, tokens, done)")
-            s.out_scores = _array(out[0], "out scores", torch.float64, (B, beam), dev)
-            s.out_parent = _array(out[1], "out parents", torch.int32, (B, beam), dev)
-            s.out_token = _array(out[2], "out tokens", torch.int32, (B, beam), dev)
+            s.out_scores = _array(out[0], "out scores", T.f64, shape, dev)
+            s.out_parent = _array(out[1], "out parents", T.i32, shape, dev)
+            s.out_token = _array(out[2], "out tokens", T.i32, shape, dev)
             if out[3] is not None:
-                _array(out[3], "out done", torch.bool, (B, beam), dev)
+                _array(out[3], "out done", T.bool, shape, dev)
         if out[3] is not None:
             s.out_done = out[3].data_ptr()
-        s.workspace_bytes = lib.rnnt_select_tokens_workspace(B, beam, V)
-        if s.workspace_bytes:
-            work = torch.empty(s.workspace_bytes, dtype=torch.uint8, device=dev)
-            s.workspace = work.data_ptr()
-        _check(lib.rnnt_select_tokens(C.byref(s), raw))
+        need = T.lib.rnnt_select_tokens_workspace(B, beam, V)
+        if need:
+            work = T.empty(need, dtype=T.u8, device=dev)
+            s.workspace, s.workspace_bytes = work.data_ptr(), need
+        _check(T.lib.rnnt_select_tokens(C.byref(s), raw))
+    finally:
+        if scope:
+            scope.close()
     return out
 
 
-def _rows_of(shape, strides, what):
+def _rows_of(shape, strides, which):
     """(rows, stride, run) of trailing dimensions: a run of contiguous elements, repeated at one stride."""
+    if len(shape) == 1 and strides[0] == 1:
+        return 1, 0, shape[0]
     run, dims = 1, list(zip(shape, strides))
     while dims and (dims[-1][0] == 1 or dims[-1][1] == run):
         run *= dims.pop()[0]
@@ -152,31 +164,35 @@ def _rows_of(shape, strides, what):
     rows, stride = dims.pop()
     while dims and dims[-1][1] == stride * rows:
         rows *= dims.pop()[0]
-    _refuse(not dims, f"{what}: the dimensions behind the slots must be one run of elements or runs at one stride")
+    _refuse(not dims, f"state {which}: the dimensions behind the slots must be one run of elements or runs at one stride")
     return rows, stride, run
 
 
 def reorder_states(parents, states, lead=0, stream=None):
     """rnnt_reorder_states: state[b, k] = state[b, parents[b, k]] in place, for each of up to 16 tensors of any type, [B, beam, ...] behind
     ``lead`` (0 or 1) dimensions, e.g. of layers.  parents int32 [B, beam]; those outside 0 .. beam - 1 leave their slot as it is."""
-    import torch
-    _refuse(parents.dim() == 2 and parents.shape[0] >= 1 and parents.shape[1] >= 1, "parents must be [B, beam]")
-    B, beam = parents.shape
-    ptr = _array(parents, "parents", torch.int32, (B, beam), parents.device)
+    T = _torch()
+    if parents.dim() != 2 or parents.numel() == 0:
+        raise RnntBeamError("parents must be [B, beam]")
+    shape, dev = parents.shape, parents.device
+    ptr = _array(parents, "parents", T.i32, shape, dev)
     _refuse(lead in (0, 1), "lead must be 0 or 1")
     _refuse(len(states) <= 16, "at most 16 tensors")
     views = (_States * max(len(states), 1))()
-    for i, (v, t) in enumerate(zip(views, states)):
-        _refuse(t.device == parents.device, f"state {i} is on {t.device}, not on {parents.device}")
-        _refuse(t.dim() >= lead + 2 and tuple(t.shape[lead:lead + 2]) == (B, beam), f"state {i} must be [{'layers, ' * lead}B, beam, ...]")
-        shape, strides, size = t.shape, t.stride(), t.element_size()
-        rows, stride, run = _rows_of(shape[lead + 2:], strides[lead + 2:], f"state {i}")
-        v.data = t.data_ptr()
-        v.lead, v.lead_stride = (shape[0], strides[0] * size) if lead else (1, 0)
-        v.b_stride, v.slot_stride = strides[lead] * size, strides[lead + 1] * size
-        v.inner, v.inner_stride, v.row_bytes = rows, stride * size, run * size
-    with _Call(parents, stream, (parents, *states)) as raw:
-        _check(load_library().rnnt_reorder_states(C.c_void_p(ptr), B, beam, views, len(states), raw))
+    for i, t in enumerate(states):
+        full, strides, size = t.shape, t.stride(), t.element_size()
+        if t.device != dev or full[lead:lead + 2] != shape:
+            _refuse(t.device == dev, f"state {i} is on {t.device}, not on {dev}")
+            raise RnntBeamError(f"state {i} must be [{'layers, ' * lead}B, beam, ...]")
+        rows, stride, run = _rows_of(full[lead + 2:], strides[lead + 2:], i)
+        outer, outer_stride = (full[0], strides[0]) if lead else (1, 0)
+        views[i] = _States(t.data_ptr(), outer_stride * size, strides[lead] * size, strides[lead + 1] * size, stride * size, run * size, outer, rows)
+    raw, scope = _enter(T, parents, stream, (parents, *states))
+    try:
+        _check(T.lib.rnnt_reorder_states(C.c_void_p(ptr), shape[0], shape[1], views, len(states), raw))
+    finally:
+        if scope:
+            scope.close()
 
 
 class KVCache:
@@ -215,49 +231,64 @@ class KVCache:
         self._c.k_exp = _array(k_exp, "k_exp", torch.uint8, tuple(k.shape[:3]), self.device)
         self._c.v_exp = _array(v_exp, "v_exp", torch.uint8, tuple(k.shape[:3]), self.device)
 
-    def _view(self, table, B):
-        import torch
-        _refuse(table.dim() == 2 and table.dtype == torch.int32 and table.shape[0] == B and table.shape[1] >= 1, f"table must be int32 [{B}, width]")
-        _refuse(table.device == self.device, f"table is on {table.device}, not on {self.device}")
-        _refuse(table.shape[1] == 1 or table.stride(1) == 1, "rows of table must be contiguous")
+    def _view(self, T, table, B):
+        shape, strides = table.shape, table.stride()
+        if len(shape) != 2 or table.dtype != T.i32 or shape[0] != B or shape[1] < 1 or table.device != self.device or (shape[1] > 1 and strides[1] != 1):
+            _refuse(len(shape) == 2 and table.dtype == T.i32 and shape[0] == B and shape[1] >= 1, f"table must be int32 [{B}, width]")
+            _refuse(table.device == self.device, f"table is on {table.device}, not on {self.device}")
+            raise RnntBeamError("rows of table must be contiguous")
         c = _Cache.from_buffer_copy(self._c)
-        c.table, c.table_stride, c.width = table.data_ptr(), table.stride(0), table.shape[1]
+        c.table, c.table_stride, c.width = table.data_ptr(), strides[0], shape[1]
         return c
 
     def _rows(self, t, what, heads):
-        _refuse(t.dim() == 4 and t.shape[2] == heads and t.shape[3] == self.dim, f"{what} must be [B, n, {heads}, {self.dim}]")
-        _refuse(t.device == self.device, f"{what} is on {t.device}, not on {self.device}")
-        _refuse(t.stride(3) == 1, f"the last dimension of {what} must be contiguous")
-        return _Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 4 or shape[2] != heads or shape[3] != self.dim or t.device != self.device or strides[3] != 1:
+            _refuse(len(shape) == 4 and shape[2] == heads and shape[3] == self.dim, f"{what} must be [B, n, {heads}, {self.dim}]")
+            _refuse(t.device == self.device, f"{what} is on {t.device}, not on {self.device}")
+            raise RnntBeamError(f"the last dimension of {what} must be contiguous")
+        return _Rows(t.data_ptr(), strides[0], strides[1], strides[2])
 
-    def _counts(self, start, count, B):
-        import torch
-        return (C.c_void_p(_array(start, "start", torch.int32, (B,), self.device)),
-                C.c_void_p(_array(count, "count", torch.int32, (B,), self.device)) if count is not None else None)
+    def _counts(self, T, start, count, B):
+        return (C.c_void_p(_array(start, "start", T.i32, (B,), self.device)),
+                C.c_void_p(_array(count, "count", T.i32, (B,), self.device)) if count is not None else None)
 
     def write(self, k, v, table, start, count=None, stream=None):
         """rnnt_cache_write: rows k, v [B, n, heads, dim] (float32, float16 or bfloat16) to positions start[b] + i, i < count[b] (None: n)."""
-        B, n = k.shape[:2]
-        _refuse(k.dtype == v.dtype and k.shape == v.shape, "k and v must have one type and shape")
-        code, c = _type_of(k, "k"), self._view(table, B)
+        T = _torch()
+        shape = k.shape
+        if k.dtype != v.dtype or shape != v.shape or len(shape) != 4:
+            raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
+        B, n = shape[0], shape[1]
+        code, c = _type_of(T, k, "k"), self._view(T, table, B)
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
-        first, many = self._counts(start, count, B)
-        with _Call(k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp)) as raw:
-            _check(load_library().rnnt_cache_write(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+        first, many = self._counts(T, start, count, B)
+        raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))
+        try:
+            _check(T.lib.rnnt_cache_write(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+        finally:
+            if scope:
+                scope.close()
 
     def read(self, table, start, n, dtype=None, count=None, stream=None):
         """rnnt_cache_read: (k, v) [B, n, heads, dim] of ``dtype`` (default float32), the rows at positions start[b] + i; zeros from count[b] on and
         where there is no page."""
-        import torch
-        dtype = dtype or torch.float32
-        B = table.shape[0]
-        c = self._view(table, B)
-        first, many = self._counts(start, count, B)
-        with _Call(self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp)) as raw:
-            out = tuple(torch.empty((B, n, self.heads, self.dim), dtype=dtype, device=self.device) for _ in range(2))
+        T = _torch()
+        dtype = dtype or T.f32
+        code, B = T.types.get(dtype), table.shape[0]
+        _refuse(code is not None, "dtype must be float32, float16 or bfloat16")
+        c = self._view(T, table, B)
+        first, many = self._counts(T, start, count, B)
+        raw, scope = _enter(T, self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp))
+        try:
+            heads, dim = self.heads, self.dim
+            out = tuple(T.empty((B, n, heads, dim), dtype=dtype, device=self.device) for _ in range(2))
             if n:
-                code, rk, rv = _type_of(out[0], "dtype"), self._rows(out[0], "k", self.heads), self._rows(out[1], "v", self.heads)
-                _check(load_library().rnnt_cache_read(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+                rk, rv = (_Rows(t.data_ptr(), n * heads * dim, heads * dim, dim) for t in out)
+                _check(T.lib.rnnt_cache_read(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+        finally:
+            if scope:
+                scope.close()
         return out
 
     def attend(self, q, table, lens, parents=None, scale=None, max_len=None, out=None, stream=None):
@@ -266,31 +297,38 @@ class KVCache:
         each sees its ancestors (-1: none) and itself; less than -1: padding.  None: each node follows the one before it, n = 1 is a step of
         a search.  ``scale``: default dim ** -0.5.  ``max_len``: a bound of lens + tree, by which work is split (default: all that
         the table holds).  Returns [B, n, q_heads, dim] of q's type; ``out``: contiguous, such a tensor to write to."""
-        import torch
-        _refuse(q.dim() == 4, "q must be [B, n, q_heads, dim]")
-        B, n, heads, dim = q.shape
-        c = self._view(table, B)
-        a = _Attend(struct_size=C.sizeof(_Attend), type=_type_of(q, "q"), B=B, n=n, tree=n, q_heads=heads,
-                    scale=dim ** -0.5 if scale is None else scale)
-        a.q = self._rows(q, "q", heads)
-        a.max_len = min(self.page_size * table.shape[1] if max_len is None else max_len, 0x7fffffff)
-        a.lens = _array(lens, "lens", torch.int32, (B,), self.device)
+        T = _torch()
+        shape = q.shape
+        if len(shape) != 4:
+            raise RnntBeamError("q must be [B, n, q_heads, dim]")
+        B, n, heads, dim = shape
+        c = self._view(T, table, B)
+        rows = self._rows(q, "q", heads)
+        bound = self.page_size * c.width if max_len is None else max_len
+        a = _Attend(C.sizeof(_Attend), _type_of(T, q, "q"), B, n, n, heads, dim ** -0.5 if scale is None else scale, min(bound, 0x7fffffff), rows)
+        a.lens = _array(lens, "lens", T.i32, (B,), self.device)
         if parents is not None:
             _refuse(parents.dim() == 2, "parents must be [B, tree]")
             a.tree = parents.shape[1]
-            a.parents = _array(parents, "parents", torch.int32, (B, a.tree), self.device)
-        lib = load_library()
-        with _Call(q, stream, (q, table, lens, parents, out, self.k, self.v, self.k_exp, self.v_exp)) as raw:
-            a.workspace_bytes = _check(lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(a)))
+            a.parents = _array(parents, "parents", T.i32, (B, a.tree), self.device)
+        lib = T.lib
+        raw, scope = _enter(T, q, stream, (q, table, lens, parents, out, self.k, self.v, self.k_exp, self.v_exp))
+        try:
+            need = lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(a))
+            if need < 0:
+                _check(need)
             if out is None:
-                out = torch.empty((B, n, heads, dim), dtype=q.dtype, device=self.device)
+                out = T.empty(shape, dtype=q.dtype, device=self.device)
                 a.out = out.data_ptr()
             else:
-                a.out = _array(out, "out", q.dtype, (B, n, heads, dim), self.device)
-            if a.workspace_bytes:
-                work = torch.empty(a.workspace_bytes, dtype=torch.uint8, device=self.device)
-                a.workspace = work.data_ptr()
+                a.out = _array(out, "out", q.dtype, shape, self.device)
+            if need:
+                work = T.empty(need, dtype=T.u8, device=self.device)
+                a.workspace, a.workspace_bytes = work.data_ptr(), need
             _check(lib.rnnt_cache_attend(C.byref(c), C.byref(a), raw))
+        finally:
+            if scope:
+                scope.close()
         return out
 
 
