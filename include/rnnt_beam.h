@@ -389,7 +389,7 @@ typedef struct {
   int32_t n_pages, page_size;  /* page_size a power of two up to 4096; n_pages * heads * page_size < 2^32 - 1,
                                   width * page_size at most 2^30 */
   int32_t heads, dim;          /* key heads; dim a multiple of 16, 16 .. 256 */
-  void *k, *v;                 /* [n_pages, heads, page_size, dim], 16-byte aligned */
+  void *k, *v;                 /* [n_pages, heads, page_size, dim], 16-byte aligned, less than 64 GiB each */
   uint8_t *k_exp, *v_exp;      /* [n_pages, heads, page_size]: s + 127 */
   const int32_t *table;        /* [B, width], rows table_stride apart */
   int64_t table_stride;

@@ -21,6 +21,7 @@ int cache_view(const rnnt_cache_t *c, CacheView &v) {
   if (c->dim < 16 || c->dim > 256 || c->dim % 16) return refuse("dim must be a multiple of 16 from 16 to 256");
   if (c->page_size < 1 || c->page_size > 4096 || (c->page_size & (c->page_size - 1))) return refuse("page_size must be a power of two up to 4096");
   if ((int64_t)c->n_pages * c->heads > 0xfffffffell / c->page_size) return refuse("n_pages * heads * page_size must be below 2^32 - 1");
+  if ((int64_t)c->n_pages * c->heads * c->page_size > 0xffffffffll / (c->dim * (c->format == RNNT_CACHE_F16 ? 2 : 1) / 16)) return refuse("k and v may have up to 64 GiB each");
   if ((int64_t)c->width * c->page_size > 1 << 30) return refuse("width * page_size must be at most 2^30");
   v.k = static_cast<char *>(c->k);
   v.v = static_cast<char *>(c->v);
@@ -97,10 +98,10 @@ int rows_call(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t
 
 // How the work of a call is cut: see attend_plan
 struct AttendPlan {
-  int dp, mt, rows, row_tiles, splits, split_len;
+  int dp, mt, rows, row_tiles, splits, split_len, join_shares;
   int64_t blocks, workspace;
 };
-int attend_plan(const CacheView &c, const rnnt_attend_t *s, AttendPlan &p) {
+int attend_plan(const CacheView &c, bool f8, const rnnt_attend_t *s, AttendPlan &p) {
   if (!s || s->struct_size != sizeof(rnnt_attend_t)) return refuse("NULL argument or struct_size mismatch");
   if (s->B < 1 || s->n < 1 || s->tree < s->n) return refuse("B and n must be at least 1, n at most tree");
   if (s->parents && s->tree > kTreeMax) return refuse("a tree with parents has at most 1024 nodes");
@@ -112,16 +113,19 @@ int attend_plan(const CacheView &c, const rnnt_attend_t *s, AttendPlan &p) {
   p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
   p.mt = rows > 16 && p.dp < 256 ? 2 : 1;
   p.row_tiles = (int)((rows + 16 * p.mt - 1) / (16 * p.mt));
-  // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for two on every unit, none shorter
+  // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for two on every unit, four where a
+  // unit holds three, none shorter
   // than 256 tokens, two tiles for each of its waves
   const int64_t room = (int64_t)c.width << c.page_shift, longest = s->max_len < room ? (s->max_len > 1 ? s->max_len : 1) : room;
-  const int64_t others = pairs * p.row_tiles, want = (2 * kUnits + others - 1) / others, most = (longest + 255) / 256;
+  const int64_t others = pairs * p.row_tiles, want = ((attend_blocks(f8 ? 8 : 16, p.dp, p.mt) > 2 ? 4 : 2) * kUnits + others - 1) / others, most = (longest + 255) / 256;
   int64_t splits = want < most ? want : most;
   int64_t len = ((longest + splits - 1) / splits + 127) / 128 * 128;
   splits = (longest + len - 1) / len;
   p.splits = (int)splits;
   p.split_len = (int)len;
   p.blocks = (pairs * splits + 7) / 8 * 8 * p.row_tiles;
+  p.join_shares = 1;  // four splits for each thread of the join
+  while (p.join_shares < 8 && p.join_shares * 4 < splits && c.dim / 4 * p.join_shares * 2 <= 256) p.join_shares *= 2;
   p.workspace = splits > 1 ? splits * pairs * rows * (int64_t)(c.dim * sizeof(float) + sizeof(float2)) : 0;
   return RNNT_OK;
 }
@@ -152,7 +156,7 @@ int64_t rnnt_cache_attend_workspace(const rnnt_cache_t *cache, const rnnt_attend
   CacheView c;
   AttendPlan p;
   if (const int rc = cache_view(cache, c)) return rc;
-  if (const int rc = attend_plan(c, s, p)) return rc;
+  if (const int rc = attend_plan(c, cache->format == RNNT_CACHE_E4M3, s, p)) return rc;
   return p.workspace;
 } catch (...) {
   return RNNT_E_NOMEM;
@@ -162,7 +166,7 @@ int rnnt_cache_attend(const rnnt_cache_t *cache, const rnnt_attend_t *s, void *h
   AttendArgs a;
   AttendPlan p;
   if (const int rc = cache_view(cache, a.c)) return rc;
-  if (const int rc = attend_plan(a.c, s, p)) return rc;
+  if (const int rc = attend_plan(a.c, cache->format == RNNT_CACHE_E4M3, s, p)) return rc;
   if (!s->q.data || !s->out || !s->lens) return refuse("NULL array");
   if (p.workspace && (!s->workspace || (uintptr_t)s->workspace % 16 || s->workspace_bytes < p.workspace))
     return refuse("workspace is missing, too small or not aligned");
@@ -181,6 +185,7 @@ int rnnt_cache_attend(const rnnt_cache_t *cache, const rnnt_attend_t *s, void *h
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
   a.split_len = p.split_len;
+  a.join_shares = p.join_shares;
   a.scale = s->scale;
   a.part = static_cast<float *>(s->workspace);
   a.stat = reinterpret_cast<float2 *>(a.part + (int64_t)p.splits * s->B * a.c.heads * p.rows * a.c.dim);

@@ -28,8 +28,9 @@ struct AttendArgs {
   int B, n, tree, group;                 // queries are the last n of `tree` nodes
   int rows, row_tiles, splits, split_len;  // split_len: tokens, a multiple of 128
   float scale;
-  float *part;   // [splits][B * heads][rows][dim]
-  float2 *stat;  // [splits][B * heads][rows]: (M, sum); a negative sum: the row's node is not there
+  float *part;      // [splits][B * heads][rows][dim]: outputs of a split's tokens
+  float2 *stat;     // [splits][B * heads][rows]: (M, sum); a negative sum: the row's node is not there
+  int join_shares;  // threads of the join for 4 values of a row
 };
 
 constexpr int kTreeMax = 1024;  // nodes of a tree with parents
@@ -58,7 +59,7 @@ __device__ __forceinline__ int reference_exp(const CacheView &c, int h, int page
 // what two values rounded to float16 leave, rounded to float16
 __device__ __forceinline__ uint32_t pack_f16_rest(float a, float b, uint32_t hi) {
   const f16x2_t h = __builtin_bit_cast(f16x2_t, hi);
-  return pack_f16(a - (float)h[0], b - (float)h[1]);
+  return pack_f16(fmaf((float)h[0], -1.f, a), fmaf((float)h[1], -1.f, b));  // (one mixed multiply-add each; exact)
 }
 
 // a pair of float16 with zeros in place of NaN and infinities
@@ -90,6 +91,16 @@ __device__ __forceinline__ void load_bytes(Bytes<N> &d, const char *p) {
   }
 }
 
+__device__ __forceinline__ int64_t out_row(const AttendArgs &a, int b, int h, int row) {
+  return (((int64_t)b * a.n + row / a.group) * (a.c.heads * a.group) + h * a.group + row % a.group) * a.c.dim;
+}
+__device__ __forceinline__ void put_output(float *p, floatx4 o) { *reinterpret_cast<floatx4 *>(p) = o; }
+__device__ __forceinline__ void put_output(_Float16 *p, floatx4 o) { *reinterpret_cast<uintx2_t *>(p) = uintx2_t{pack_f16(o[0], o[1]), pack_f16(o[2], o[3])}; }
+__device__ __forceinline__ void put_output(uint16_t *p, floatx4 o) { *reinterpret_cast<uintx2_t *>(p) = uintx2_t{pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])}; }
+
+// blocks of four waves that a compute unit holds, one wave of each on a SIMD: what the registers allow
+constexpr int attend_blocks(int fmt, int dp, int mt) { return mt > 1 ? 2 : dp == 64 ? 4 : dp == 128 && fmt == 8 ? 3 : 2; }
+
 template <typename TT, int FMT, int DP, int MT>
 struct Attend {
   typedef typename TT::T T;
@@ -115,16 +126,13 @@ struct Attend {
     uint8_t gone[MT * 16];
   };
   struct Meta {  // of a wave's tile of 32 tokens
-    uint32_t row[32];
+    uint32_t at[32];  // of the tokens' rows, in 16 bytes
     float k_scale[32], v_exp[32], v_inv[32];
   };
   // a lane's part of a tile: key rows l16 and 16 + l16, and its dims of eight value rows
   typedef Bytes<KQ * FB> Keys[2];
   typedef Bytes<VN * FB> Values[8];
-  // Tiles in registers: two, one on its way while the other is multiplied, where they are small enough for two blocks of a unit; else one, whose
-  // keys are followed by the next ones when they have been multiplied, and its values likewise.
-  static constexpr int BUFS = DP * FB <= 64 ? 2 : 1;
-  static constexpr int WAVES = DP == 64 && MT == 1 ? (FMT == 8 ? 4 : 3) : DP == 128 && MT == 1 && FMT == 8 ? 3 : 2;
+  static constexpr int WAVES = attend_blocks(FMT, DP, MT);
 };
 
 template <typename TT, int FMT, int DP, int MT>
@@ -138,7 +146,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
 
   // Blocks of the same tokens on one XCD, one after the other (block i runs on XCD i % 8); first splits first: which of the later ones have work
-  // hangs on the lengths, and with the splits of a sequence side by side some XCDs had those that do not (32 sequences of 1000 to 8000 tokens: 78 us)
+  // hangs on the lengths, and with the splits of a sequence side by side some XCDs had those that do not (32 sequences of 1000 to 8000 tokens: 78 us, now 66)
   const int groups = a.B * c.heads * a.splits;
   const int per = 8 * a.row_tiles, slab = blockIdx.x / per, in = blockIdx.x - slab * per;
   const int item = slab * 8 + (in & 7), tile_r = in >> 3;
@@ -189,10 +197,11 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
 
   typename A::Meta &mt = meta[wave];
   // Where a lane's part of a row lies: a lane whose dims a row does not have reads the first ones, against zeros of Q or for nothing.
-  int k_off[KQ * FB / 16];
+  const char *k_from[KQ * FB / 16];
 #pragma unroll
-  for (int j = 0; j < KQ * FB / 16; ++j) k_off[j] = 64 * j + 16 * g4 < D * FB ? 64 * j + 16 * g4 : 0;
-  const int v_off = l16 * VN < D ? l16 * VN * FB : 0, row_bytes = D * FB;
+  for (int j = 0; j < KQ * FB / 16; ++j) k_from[j] = c.k + (64 * j + 16 * g4 < D * FB ? 64 * j + 16 * g4 : 0);
+  const char *const v_from = c.v + (l16 * VN < D ? l16 * VN * FB : 0);
+  const int row_bytes = D * FB;
   // Loads are never left out: those of tokens that are not there read row 0 of the cache.  A load behind a branch would make every wait one for all
   // loads under way, the next tile's among them.
   struct Head {  // lanes 0..31 and 32..63: the 32 tokens of a tile; row, exponent of K's row (lanes 32..63: of V's)
@@ -209,7 +218,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
     o.there = t < t_end && (unsigned)page < (unsigned)c.n_pages;
     o.row = o.there ? (((uint32_t)page * c.heads + h) << c.page_shift) + (t & (c.page_size - 1)) : 0u;
     wave_lds_order();
-    if (lane < 32) mt.row[lane] = o.row;
+    if (lane < 32) mt.at[lane] = o.row * (uint32_t)(row_bytes >> 4);
     wave_lds_order();
     o.e = exps[o.row];
     return o;
@@ -217,11 +226,11 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   auto load_keys = [&](typename A::Keys &keys) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const char *p = c.k + (uint64_t)mt.row[16 * i + l16] * (uint32_t)row_bytes;
+      const uint64_t at = (uint64_t)mt.at[16 * i + l16] << 4;
 #pragma unroll
       for (int j = 0; j < KQ * FB / 16; ++j) {
         Bytes<16> part;
-        load_bytes(part, p + k_off[j]);
+        load_bytes(part, k_from[j] + at);
 #pragma unroll
         for (int w = 0; w < 4; ++w) keys[i].w[4 * j + w] = part.w[w];
       }
@@ -229,22 +238,22 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   };
   auto load_values = [&](typename A::Values &values) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) load_bytes(values[j], c.v + (uint64_t)mt.row[(j >> 2) * 16 + 4 * g4 + (j & 3)] * (uint32_t)row_bytes + v_off);
+    for (int j = 0; j < 8; ++j) load_bytes(values[j], v_from + ((uint64_t)mt.at[(j >> 2) * 16 + 4 * g4 + (j & 3)] << 4));
   };
 
   // ---- the first tile's loads leave ahead of everything that does not need them
   int t0 = t_begin + wave * 32;
   const bool busy = t0 < t_end;
-  typename A::Keys keys[A::BUFS];
-  typename A::Values values[A::BUFS];
+  typename A::Keys keys;
+  typename A::Values values;
   Head head[2] = {};
   int page_next = 0;
   if (busy) {
     const int page = page_of(t0);
     page_next = page_of(t0 + 128);
     head[0] = head_of(t0, page);
-    load_keys(keys[0]);
-    load_values(values[0]);
+    load_keys(keys);
+    load_values(values);
   }
   const int e0 = reference_exp(c, h, ref_page, total);
 
@@ -455,33 +464,14 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   };
 
   if (busy) {
-    if constexpr (A::BUFS == 2) {
-      const auto nothing = [] {};
-      while (true) {
-        head[1] = head_of(t0 + 128, page_next);
-        load_keys(keys[1]);
-        load_values(values[1]);
-        page_next = page_of(t0 + 256);
-        take_tile(t0, head[0], keys[0], values[0], nothing, nothing);
-        t0 += 128;
-        if (t0 >= t_end) break;
-        head[0] = head_of(t0 + 128, page_next);
-        load_keys(keys[0]);
-        load_values(values[0]);
-        page_next = page_of(t0 + 256);
-        take_tile(t0, head[1], keys[1], values[1], nothing, nothing);
-        t0 += 128;
-        if (t0 >= t_end) break;
-      }
-    } else {
-      do {
-        head[1] = head_of(t0 + 128, page_next);
-        page_next = page_of(t0 + 256);
-        take_tile(t0, head[0], keys[0], values[0], [&] { load_keys(keys[0]); }, [&] { load_values(values[0]); });
-        head[0] = head[1];
-        t0 += 128;
-      } while (t0 < t_end);
-    }
+    // one tile in registers, whose keys are followed by the next ones when they have been multiplied, and its values likewise
+    do {
+      head[1] = head_of(t0 + 128, page_next);
+      page_next = page_of(t0 + 256);
+      take_tile(t0, head[0], keys, values, [&] { load_keys(keys); }, [&] { load_values(values); });
+      head[0] = head[1];
+      t0 += 128;
+    } while (t0 < t_end);
   }
 
   // ---- the four waves' shares
@@ -516,80 +506,69 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = fmaf(f, sh.o[w][r][d + j], o[j]);
     }
-    const bool gone = treed && sh.gone[r];
-    if (a.splits > 1) {
-      if (d == 0) a.stat[part_row + row] = make_float2(m_all, gone ? -1.f : l);
-      if (d < D) *reinterpret_cast<floatx4 *>(a.part + (part_row + row) * D + d) = o;
-    } else if (d < D) {
-      const int node = row / a.group, head_i = h * a.group + row % a.group;
-      T *out = static_cast<T *>(a.out) + (((int64_t)b * a.n + node) * (c.heads * a.group) + head_i) * D + d;
-      const float inv = gone || l == 0.f ? 0.f : 1.f / l;
-      const float back = gone || l == 0.f ? 0.f : ldexpf(1.f, e0 - 127);
+    const bool gone = treed && sh.gone[r], none = gone || l == 0.f;
+    const float inv = 1.f / l, back = ldexpf(1.f, e0 - 127);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float y = back == 0.f ? 0.f : o[j] * inv * back;
-        if constexpr (std::is_same<T, uint16_t>::value) out[j] = (uint16_t)pack_bf16_rne(y, y);
-        else out[j] = (T)y;
-      }
-    }
+    for (int j = 0; j < 4; ++j) o[j] = none ? 0.f : o[j] * inv * back;
+    if (a.splits > 1 && d == 0) a.stat[part_row + row] = make_float2(m_all, gone ? -1.f : l);
+    if (d >= D) continue;
+    if (a.splits == 1) put_output(static_cast<T *>(a.out) + out_row(a, b, h, row) + d, o);
+    else *reinterpret_cast<floatx4 *>(a.part + (part_row + row) * D + d) = o;
   }
 }
 
-// ---- shares of the splits of a row: a block for each row, dim / 4 lanes for a share, as many shares at a time as the block has room for
+// ---- the splits of a row: `join_shares` threads for 4 values of it, each a split at a time
 template <typename TT>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   typedef typename TT::T T;
   __shared__ floatx4 sh_o[256];
-  __shared__ float sh_l;
+  __shared__ float2 sh_s[256];
   const CacheView &c = a.c;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = c.dim, lanes = D / 4, shares = 256 / lanes;
-  const int64_t all = (int64_t)a.B * c.heads * a.rows, at = blockIdx.x;
-  const int bh = (int)(at / a.rows), row = (int)(at - (int64_t)bh * a.rows), b = bh / c.heads, h = bh - b * c.heads;
-  const int ref_page = reference_page(c, b);
-  const int64_t room = (int64_t)c.width << c.page_shift;
-  const int total = (int)min((int64_t)max(a.lens[b], 0) + a.tree, room);
-  const int used = min(a.splits, (total + a.split_len - 1) / a.split_len);
-  const int e0 = reference_exp(c, h, ref_page, total);
-  // every wave all of the maxima, their sum and its own shares' factors
-  float m_all = kMStart, l = 0.f;
-  bool gone = false;
-  for (int s = lane; s < used; s += 64) {
-    const float2 st = a.stat[s * all + at];
-    m_all = fmaxf(m_all, st.x);
-    gone |= st.y < 0.f;
-  }
-  m_all = wave_max(m_all);
-  const int mine = threadIdx.x / lanes, d = threadIdx.x % lanes * 4;
+  const int D = c.dim, lanes = D / 4, per_row = lanes * a.join_shares, rows = 256 / per_row;
+  const int64_t all = (int64_t)a.B * c.heads * a.rows;
+  const int r = threadIdx.x / per_row, mine = threadIdx.x % per_row / lanes, d = threadIdx.x % lanes * 4;
+  const int64_t at = (int64_t)blockIdx.x * rows + r;
+  const bool there = r < rows && at < all;
+  const int bh = there ? (int)(at / a.rows) : 0, b = bh / c.heads;
+  float m = kMStart, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  if (mine < shares) {
+  bool gone = false;
+  if (there) {
+    const int64_t total = min((int64_t)max(a.lens[b], 0) + a.tree, (int64_t)c.width << c.page_shift);
+    const int used = (int)min((int64_t)a.splits, (total + a.split_len - 1) / a.split_len);
 #pragma unroll 4
-    for (int s = mine; s < used; s += shares) {
-      const float f = __builtin_amdgcn_exp2f(a.stat[s * all + at].x - m_all);
-      o += f * *reinterpret_cast<const floatx4 *>(a.part + (s * all + at) * D + d);
-    }
-  }
-  if (wave == 0) {
-    for (int s = lane; s < used; s += 64) {
-      const float2 st = a.stat[s * all + at];
-      l = fmaf(__builtin_amdgcn_exp2f(st.x - m_all), st.y, l);
-    }
-    l = __any(gone) ? 0.f : wave_sum(l);
-    if (lane == 0) sh_l = l;
-  }
-  sh_o[threadIdx.x] = o;
-  __syncthreads();
-  if (threadIdx.x >= lanes) return;
-  for (int s = 1; s < shares && s < used; ++s) o += sh_o[s * lanes + threadIdx.x];
-  l = sh_l;
-  const int node = row / a.group, head_i = h * a.group + row % a.group;
-  T *out = static_cast<T *>(a.out) + (((int64_t)b * a.n + node) * (c.heads * a.group) + head_i) * D + d;
-  const float inv = 1.f / l, back = ldexpf(1.f, e0 - 127);
+    for (int s = mine; s < used; s += a.join_shares) {
+      const int64_t from = s * all + at;
+      const float2 st = a.stat[from];
+      const floatx4 part = *reinterpret_cast<const floatx4 *>(a.part + from * D + d);
+      gone |= st.y < 0.f;
+      const float m_new = fmaxf(m, st.x), keep = __builtin_amdgcn_exp2f(m - m_new), add = st.y * __builtin_amdgcn_exp2f(st.x - m_new);
+      l = fmaf(l, keep, add);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float y = l == 0.f ? 0.f : o[j] * inv * back;
-    if constexpr (std::is_same<T, uint16_t>::value) out[j] = (uint16_t)pack_bf16_rne(y, y);
-    else out[j] = (T)y;
+      for (int j = 0; j < 4; ++j) o[j] = fmaf(o[j], keep, add * part[j]);
+      m = m_new;
+    }
   }
+  if (a.join_shares > 1) {
+    sh_o[threadIdx.x] = o;
+    sh_s[threadIdx.x] = make_float2(m, gone ? -1.f : l);
+    __syncthreads();
+    if (mine) return;
+    for (int i = 1; there && i < a.join_shares; ++i) {
+      const float2 st = sh_s[threadIdx.x + i * lanes];
+      gone |= st.y < 0.f;
+      const float m_new = fmaxf(m, st.x), keep = __builtin_amdgcn_exp2f(m - m_new), add = __builtin_amdgcn_exp2f(st.x - m_new);
+      l = fmaf(l, keep, add * st.y);
+      o = o * keep + sh_o[threadIdx.x + i * lanes] * add;
+      m = m_new;
+    }
+  }
+  if (!there) return;
+  const bool none = gone || l == 0.f;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = none ? 0.f : o[j] * inv;
+  put_output(static_cast<T *>(a.out) + out_row(a, b, bh - b * c.heads, (int)(at - (int64_t)bh * a.rows)) + d, o);
 }
 
 }  // namespace rb
