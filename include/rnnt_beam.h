@@ -328,7 +328,7 @@ int rnnt_beam_kernel_times(rnnt_beam_t *h, const char **names, float *ms, int32_
 /* ---------------------------------------------------------------------------------------------------------------
  * Operators for networks that the caller runs itself: an attention decoder searched with a beam, a neural language model that rescores the
  * n-best lists of a decode.  The caller computes the products; these calls keep its keys and values, attend over them, select the tokens
- * and move the states of hypotheses.  All pointers are device memory unless stated; work is enqueued on hip_stream and the calls return at
+ * and move the states of hypotheses.  All pointers are memory of the current device unless stated; work is enqueued on hip_stream and the calls return at
  * once; nothing is allocated, no call waits, all may be captured into a HIP graph.  Structures are plain data, versioned by struct_size;
  * strides count elements (of rnnt_states_t: bytes).  RNNT_E_ARG with a message (rnnt_beam_last_error(NULL), of this thread) for what the host
  * can see to be wrong; what only the device sees (tables, lengths, parents, counts) is taken as described at each call, never beyond the arrays.
@@ -338,7 +338,8 @@ typedef enum { RNNT_TYPE_F32 = 0, RNNT_TYPE_F16 = 1, RNNT_TYPE_BF16 = 2 } rnnt_t
 /*
  * One step of a beam search over logits: for each of B utterances the `beam` best of the beam * V candidates
  *   key(k, v) = scores[k] + x[k, v] - log sum_u exp x[k, u],
- * key descending, of equal keys the smaller k V + v first.  Keys are float64, the sums of the exponentials too.  No candidates: keys of NaN or
+ * key descending, of equal keys the smaller k first, of one hypothesis' the larger logit, then the smaller v.  Keys are float64, the sums of the
+ * exponentials too (logits that differ may have one key).  No candidates: keys of NaN or
  * -inf, so none of an empty slot (score -inf), none of a row with a NaN or +inf.  A hypothesis with done[k] has one candidate, token eos
  * with key scores[k]; its logits are not read.  Outputs per slot: the key, the parent slot and the token; empty slots behind the last candidate: -inf, -1,
  * -3 (as rnnt_beam_dump_tree has them); out_done = token == eos.  scores and out_scores may be one array, done and out_done too.
@@ -346,7 +347,7 @@ typedef enum { RNNT_TYPE_F32 = 0, RNNT_TYPE_F16 = 1, RNNT_TYPE_BF16 = 2 } rnnt_t
 typedef struct {
   uint32_t struct_size;
   int32_t type;              /* of the logits, rnnt_type_t */
-  int32_t B, beam, V;        /* beam <= 16, beam * V < 2^31 */
+  int32_t B, beam, V;        /* beam <= 16, beam * V at most 2^31 - 2^16 */
   int32_t eos;               /* -1: none; done and out_done are NULL then */
   const void *logits;        /* [B, beam, V], the last dimension contiguous, rows at any address of their type */
   int64_t stride_b, stride_k;
@@ -414,8 +415,8 @@ int rnnt_cache_read(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_
  * (one token, or a chunk).  Queries are the last n nodes (n = tree: all; fewer where rows of earlier nodes are in the cache but not asked for).
  * A node whose parent is neither -1 nor a node before it is padding: its output, and that of nodes below it, is zero, its rows need not
  * have been written.  A query that sees nothing gets zeros; one that sees a row of NaN, or is not finite itself, NaN.  Rows that a query does not see
- * have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; the value rows of a
- * sequence's head, those of zeros aside, are taken as within 2^100 of the first 64 of them.  Outputs repeat bit for bit.
+ * have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; logits are taken as
+ * within 1e30, the value rows of a sequence's head, those of zeros aside, as within 2^100 of the first 64 of them.  Outputs repeat bit for bit.
  */
 typedef struct {
   uint32_t struct_size;

@@ -67,7 +67,7 @@ int rnnt_select_tokens(const rnnt_select_t *s, void *hip_stream) try {
   if (!s->logits || !s->scores || !s->out_scores || !s->out_parent || !s->out_token) return refuse("NULL array");
   if (s->B < 1 || s->V < 1) return refuse("B and V must be at least 1");
   if (s->beam < 1 || s->beam > kMaxBeam) return refuse("beam must be 1 to 16");
-  if ((int64_t)s->beam * s->V > 0x7fffffff) return refuse("beam * V must be below 2^31");
+  if ((int64_t)s->beam * s->V > 0x7fff0000) return refuse("beam * V must be at most 2^31 - 2^16");
   if (s->eos < -1 || s->eos >= s->V) return refuse("eos must be a token, or -1");
   if (s->eos < 0 && (s->done || s->out_done)) return refuse("done needs eos");
   if (s->eos >= 0 && !s->out_done) return refuse("out_done is missing");

@@ -226,6 +226,8 @@ struct SelJoin {
   double key[kSelLists][kMaxBeam + 1];  // of the lists' candidates
   double cand_key[kSelLists * kMaxBeam];
   int cand_at[kSelLists * kMaxBeam];
+  float cand_x[kSelLists * kMaxBeam];  // their logits
+  uint8_t cand_k[kSelLists * kMaxBeam];
   double sum[kSelLists];
   float ref[kSelLists];
   int n;
@@ -233,7 +235,7 @@ struct SelJoin {
 
 // One wave: the `beam` best of an utterance from the lists of its rows, lane l's being list l = k * parts + p.  A bound that they reach is the
 // beam-th largest of the first few of every list; each lane hands on those of its list that reach it, and they are
-// ranked by (key descending, flat index ascending).
+// ranked by (key descending, hypothesis, logit descending, token): lists hold the largest logits, whose keys may round to one float64.
 __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const SelList *lists, const SelStat *stats, SelJoin &sh) {
   const int lane = threadIdx.x & 63, beam = a.beam, parts = a.parts, n_lists = beam * parts;
   const int l = min(lane, n_lists - 1), k = l / parts;
@@ -268,6 +270,7 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
   if (finished && lane == k * parts) {  // its one candidate: eos, with the score that it has
     key[0] = score == score ? score : -INFINITY;
     i[0] = a.eos;
+    v[0] = 0.f;
   }
 #pragma unroll
   for (int j = 0; j < kMaxBeam; ++j) sh.key[lane][j] = key[j];
@@ -276,7 +279,7 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
   // the bound, in float32 rounded down
   const int firsts = max(min(64, 4 * beam) / n_lists, 1), list = lane / firsts;
   const double one = list < n_lists ? sh.key[list][lane - list * firsts] : -INFINITY;
-  const float low = one > -INFINITY ? from_orderable(orderable((float)one) - 1) : -INFINITY;
+  const float low = (float)one > -INFINITY ? from_orderable(orderable((float)one) - 1) : -INFINITY;  // (-inf for what float32 has no number for)
   int before = 0;
 #pragma unroll 8
   for (int j = 0; j < n_lists * firsts; ++j) before += readlane_f(low, j) > low;
@@ -291,6 +294,8 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
       if (j < mine) {
         sh.cand_key[pos + j] = key[j];
         sh.cand_at[pos + j] = k * a.V + i[j];
+        sh.cand_x[pos + j] = v[j];
+        sh.cand_k[pos + j] = (uint8_t)k;
       }
   }
   wave_lds_order();
@@ -303,21 +308,28 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     a.out_token[out + r] = token;
     if (a.out_done) a.out_done[out + r] = token == a.eos;
   };
+  const auto first_of_equals = [](int k1, float x1, int flat1, int k2, float x2, int flat2) { return k1 == k2 && x1 != x2 ? x1 > x2 : flat1 < flat2; };
   if (n <= 64) {
     const double key = lane < n ? sh.cand_key[lane] : -INFINITY;
-    const int flat = lane < n ? sh.cand_at[lane] : 0x7fffffff;
+    const int flat = lane < n ? sh.cand_at[lane] : 0x7fffffff, row = lane < n ? sh.cand_k[lane] : -1;
+    const float x = lane < n ? sh.cand_x[lane] : 0.f;
     int r = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) r += comes_before_count(readlane_d(key, j), __builtin_amdgcn_readlane(flat, j), key, flat);
+    for (int j = 0; j < n; ++j) {
+      const double other = readlane_d(key, j);
+      r += other > key;
+      if (__popcll(__ballot(other == key)) > 1)
+        r += other == key && first_of_equals(__builtin_amdgcn_readlane(row, j), readlane_f(x, j), __builtin_amdgcn_readlane(flat, j), row, x, flat);
+    }
     if (lane < n && r < beam) put(r, key, flat);
   } else {
     for (int c = lane; c < n; c += 64) {
       const double key = sh.cand_key[c];
-      const int flat = sh.cand_at[c];
       int r = 0;
 #pragma unroll 4
-      for (int j = 0; j < n; ++j) r += comes_before_count(sh.cand_key[j], sh.cand_at[j], key, flat);
-      if (r < beam) put(r, key, flat);
+      for (int j = 0; j < n; ++j)
+        r += sh.cand_key[j] > key || (sh.cand_key[j] == key && first_of_equals(sh.cand_k[j], sh.cand_x[j], sh.cand_at[j], sh.cand_k[c], sh.cand_x[c], sh.cand_at[c]));
+      if (r < beam) put(r, key, sh.cand_at[c]);
     }
   }
   for (int r = n + lane; r < beam; r += 64) {  // empty slots

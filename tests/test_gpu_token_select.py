@@ -168,6 +168,16 @@ def test_values_far_from_zero():
     check(logits, scores)
 
 
+@pytest.mark.parametrize("V", [60, 9000])
+def test_scores_that_float32_does_not_hold(V):
+    logits, _ = make(4, 4, V, "f32", 12)
+    # (next to such a score a logit is nothing: the keys of a hypothesis are equal, its largest logits win)
+    scores = np.array([[-1e300, -2e300, -3e300, -4e300], [-1e39, -1e300, -5.0, -1e40], [1e300, 2e300, 1e39, -1e39], [-np.inf, -1e300, -np.inf, -1e300]])
+    got = check(logits, scores)
+    assert got[1][0].tolist() == [0] * 4 and got[1][1].tolist() == [2] * 4
+    assert got[2][0].tolist() == logits[0, 0].topk(4).indices.tolist()
+
+
 def test_in_place_and_on_another_stream():
     import torch
     from paper_2506_00185_amd import select_tokens

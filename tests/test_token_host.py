@@ -75,7 +75,7 @@ def a_select(**over):
 
 @pytest.mark.parametrize("over,what", [
     (dict(struct_size=8), "struct_size"), (dict(type=3), "type"), (dict(type=-1), "type"), (dict(B=0), "B and V"), (dict(V=0), "B and V"), (dict(beam=0), "beam"),
-    (dict(beam=17), "beam"), (dict(beam=16, V=1 << 27), "2^31"), (dict(eos=100), "eos"), (dict(eos=-2), "eos"), (dict(eos=3), "out_done"),
+    (dict(beam=17), "beam"), (dict(beam=16, V=1 << 27), "2^31"), (dict(beam=1, V=0x7fffffff), "2^31"), (dict(beam=2, V=0x3fff8001), "2^31"), (dict(eos=100), "eos"), (dict(eos=-2), "eos"), (dict(eos=3), "out_done"),
     (dict(done=FAKE), "done"), (dict(out_done=FAKE), "done"), (dict(logits=None), "NULL"), (dict(scores=None), "NULL"), (dict(out_token=None), "NULL"),
     (dict(V=1 << 20, workspace=None), "workspace"), (dict(V=1 << 20, workspace_bytes=100), "workspace"), (dict(V=1 << 20, workspace=FAKE + 8), "workspace")])
 def test_selection_refuses(lib, over, what):

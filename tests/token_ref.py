@@ -32,7 +32,8 @@ def select(logits, scores, done=None, eos=-1):
             keys[k] = scores[b, k] + (x - (top + math.log(np.exp(x - top).sum())))
         flat = keys.reshape(-1)
         flat = np.where(np.isnan(flat), -np.inf, flat)
-        order = np.argsort(-flat, kind="stable")[:K]
+        # of equal keys the smaller hypothesis, the larger logit (keys of two may round to one), the smaller token
+        order = np.lexsort((np.arange(K * V), -np.nan_to_num(logits[b].reshape(-1)), np.repeat(np.arange(K), V), -flat))[:K]
         for r, at in enumerate(order):
             if flat[at] > -np.inf:
                 out[0][b, r], out[1][b, r], out[2][b, r], out[3][b, r] = flat[at], at // V, at % V, at % V == eos
