@@ -43,15 +43,26 @@ __device__ __forceinline__ uint32_t e4m3_lo(uint32_t w) { return __builtin_bit_c
 __device__ __forceinline__ uint32_t e4m3_hi(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, true)); }
 
 // Value exponents are taken relative to one of the sequence's first rows, so that the sums of a block stay far from float32's ends: the first that
-// tells anything (zero rows have kExpZero).  One call per wave; the same for all blocks of a sequence's head.
+// tells anything (zero rows have kExpZero; padding nodes, and those below them, hold anything).  One call per wave; the same for all blocks of a
+// sequence's head.
 __device__ __forceinline__ int reference_page(const CacheView &c, int b) {  // of the lane's token, the lane-th
   return c.table[b * c.table_stride + min((int)(threadIdx.x & 63) >> c.page_shift, c.width - 1)];
 }
-__device__ __forceinline__ int reference_exp(const CacheView &c, int h, int page, int total) {
+__device__ __forceinline__ int reference_exp(const AttendArgs &a, int b, int h, int page, int len, int total) {
+  const CacheView &c = a.c;
   const int lane = threadIdx.x & 63;
-  const bool there = lane < total && (unsigned)page < (unsigned)c.n_pages;
+  bool there = lane < total && (unsigned)page < (unsigned)c.n_pages;
   const uint32_t row = there ? (((uint32_t)page * c.heads + h) << c.page_shift) + (lane & (c.page_size - 1)) : 0u;
   const int e = c.v_exp[row];
+  if (a.parents && len < 64) {
+    const int node = lane - len, p = node >= 0 && node < a.tree ? a.parents[(int64_t)b * a.tree + node] : -1;
+    int padding = p < -1 || p >= max(node, 0), up = padding || p < 0 ? lane : len + p;
+    for (int i = 0; i < 6; ++i) {  // (64 nodes: twice as far up each time)
+      padding |= __shfl(padding, up);
+      up = __shfl(up, up);
+    }
+    there = there && !padding;
+  }
   const uint64_t good = __ballot(there && e != kExpZero && e != kExpNaN);
   return good ? __builtin_amdgcn_readlane(e, __ffsll((unsigned long long)good) - 1) : kExpZero;
 }
@@ -179,11 +190,14 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   const int len = max(a.lens[b], 0);
   const int total = (int)min((int64_t)len + a.tree, room);
   const int t_begin = (int)min((int64_t)split * a.split_len, (int64_t)total);
-  const int t_end = split + 1 < a.splits ? (int)min((int64_t)t_begin + a.split_len, (int64_t)total) : total;
-  if (split && t_begin >= t_end) return;
+  const int t_split = split + 1 < a.splits ? (int)min((int64_t)t_begin + a.split_len, (int64_t)total) : total;
+  if (split && t_begin >= t_split) return;
 
   const int first_q = a.tree - a.n;  // node of query 0
-  const bool treed = a.parents && t_end > t_begin && (t_end > len || t_end == total);
+  const bool treed = a.parents && t_split > t_begin && (t_split > len || t_split == total);
+  // no row of the block sees a node behind its last one's
+  const int last_node = first_q + min((row0 + MT * 16 - 1) / a.group, a.n - 1);
+  const int t_end = (int)min((int64_t)len + last_node + 1, (int64_t)t_split);
 
   floatx4 acc[MT][VN];
   float M[MT], sum[MT];
@@ -255,7 +269,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
     load_keys(keys);
     load_values(values);
   }
-  const int e0 = reference_exp(c, h, ref_page, total);
+  const int e0 = reference_exp(a, b, h, ref_page, len, total);
 
   {
     const int r = row0 + q_tile * 16 + l16;

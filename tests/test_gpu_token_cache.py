@@ -385,6 +385,50 @@ def test_rows_that_a_query_does_not_see_do_not_matter(fmt):
     assert torch.isnan(got[1, :7]).all() and not got[1, 7].any()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("kept", [0, 3])
+def test_padding_ahead_of_the_nodes(fmt, kept):
+    """The first rows that a sequence has are padding's, and those of nodes below it, which hold anything; the tokens kept before are zeros."""
+    import torch
+    g = np.random.default_rng(21)
+    cache, table = filled(g, 2, 100, 2, 64, fmt, 16)
+    parents = np.array([[-2, 0, -1, 1, 2, 3, 2], [-1, 0, 1, 2, 3, 4, 5]])
+    lens = np.array([kept, kept])
+    zero = torch.zeros(2, 4, 2, 64, device="cuda")
+    cache.write(zero, zero, table, cuda(np.zeros(2, np.int32)), cuda(lens.astype(np.int32)))
+    q = cuda(g.standard_normal((2, 7, 4, 64)), torch.float32)
+    first = check(cache, table, q, lens, parents)
+    for e in (0, 254):
+        for node in (0, 1, 3, 5):
+            pos = kept + node
+            page, place = int(table[0, pos // 16]), pos % 16
+            for t, x in ((cache.k, cache.k_exp), (cache.v, cache.v_exp)):
+                t.view(torch.uint8 if fmt == "e4m3" else torch.int16)[page, :, place] = 0x7E if fmt == "e4m3" else 0x7BFF
+                x[page, :, place] = e
+        assert torch.equal(first, cache.attend(q, table, cuda(lens.astype(np.int32)), cuda(parents.astype(np.int32))))
+
+
+@pytest.mark.parametrize("n,group,length", [(257, 1, 0), (100, 3, 45), (700, 2, 1300)])
+def test_chunks_of_many_tiles(n, group, length):
+    """Tiles of rows that see different numbers of the chunk's nodes; what they do not see is NaN in a second run."""
+    import torch
+    g = np.random.default_rng(n)
+    cache, table = filled(g, 2, length + n, 2, 64, "e4m3", 16, uneven=0.3)
+    q = cuda(g.standard_normal((2, n, 2 * group, 64)), torch.float32)
+    lens = np.array([length, length // 2])
+    first = check(cache, table, q, lens)
+    half = n // 2
+    nan = torch.full((2, n - half, 2, 64), float("nan"), device="cuda")
+    cache.write(nan, nan, table, cuda((lens + half).astype(np.int32)))
+    got = cache.attend(q, table, cuda(lens.astype(np.int32)))
+    assert torch.equal(got[:, :half], first[:, :half]) and torch.isnan(got[:, half:]).all()
+    # the last nodes as queries
+    tree = np.arange(n) - 1
+    if n <= 1024:
+        cache, table = filled(g, 2, length + n, 2, 64, "e4m3", 16, uneven=0.3)
+        check(cache, table, q[:, :33], lens, np.stack([tree, tree]))
+
+
 def test_pages_that_are_not_there_are_not_attended():
     import torch
     g = np.random.default_rng(11)
