@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   // hangs on the lengths, and with the splits of a sequence side by side some XCDs had those that do not (32 sequences of 1000 to 8000 tokens: 78 us, now 66)
   const int groups = a.B * c.heads * a.splits;
   const int per = 8 * a.row_tiles, slab = blockIdx.x / per, in = blockIdx.x - slab * per;
-  const int item = slab * 8 + (in & 7), tile_r = in >> 3;
+  const int item = slab * 8 + (in & 7), tile_r = a.row_tiles - 1 - (in >> 3);  // the longest first
   if (item >= groups) return;
   const int pairs = a.B * c.heads, split = item / pairs, bh = item - split * pairs, b = bh / c.heads, h = bh - b * c.heads;
   const int row0 = tile_r * MT * 16;
