@@ -8,60 +8,67 @@ namespace rb {
 // ---- soft-max statistics in float64
 // The keys of an utterance's hypotheses are compared with each other, and the sums of rows decide between candidates whose logits differ by
 // little: float32 exponentials leave 1e-8 to 1e-7 of a row's log sum open.  float64 multiply-adds run at the rate of float32 ones here, so
-// the exponential is a polynomial in float64: 2^t = 2^n 2^f, n = t rounded, and for 2^f the polynomial of degree 7 through the
-// Chebyshev points of [-1/2, 1/2], off by at most 5.5e-11 of its value.  (Sums that are brought to a common reference are multiplied by
-// the library's exp, or that error would count again.)
-__device__ __forceinline__ double exp2_d(double t) {
-  t = fmax(t, -3000.);  // of -inf too: 0
-  const double n = __builtin_rint(t), f = t - n;
-  double p = 1.5303699794189107e-05;
-  p = fma(p, f, 0.0001546972916352668);
-  p = fma(p, f, 0.0013333478479379338);
-  p = fma(p, f, 0.009618025613514537);
-  p = fma(p, f, 0.05550410906315832);
-  p = fma(p, f, 0.2402265121349604);
-  p = fma(p, f, 0.693147180556837);
-  p = fma(p, f, 0.9999999999595622);
-  return __builtin_amdgcn_ldexp(p, (int)n);
+// the exponential is a polynomial in float64: e^d = 2^n e^f with n = d / ln 2 rounded, and for e^f the polynomial of degree 7 through the
+// Chebyshev points of [-ln 2 / 2, ln 2 / 2], off by at most 5.5e-11 of its value.  Of float64 only sums and multiply-adds run at that rate: n is
+// read from the last bits of d / ln 2 + 1.5 2^52 and added to the exponent of e^f, in place of instructions that round, convert and scale.
+// (Sums that are brought to a common reference are multiplied by the library's exp, or that error would count again.)
+__device__ __forceinline__ double exp_d(double d) {  // d up to 700
+  constexpr double kRound = 6755399441055744.;
+  d = fmax(d, -690.);  // (of -inf too: e^-690 is nothing beside the 1 of the largest)
+  const double s = fma(d, kLog2E, kRound), f = fma(s - kRound, -0.6931471805599453, d);
+  double p = 0.00019907569324365478;
+  p = fma(p, f, 0.0013948578338419519);
+  p = fma(p, f, 0.008333283538688176);
+  p = fma(p, f, 0.0416662183191124);
+  p = fma(p, f, 0.1666666678630866);
+  p = fma(p, f, 0.500000010772923);
+  p = fma(p, f, 0.999999999995509);
+  p = fma(p, f, 0.9999999999595617);
+  return __hiloint2double(__double2hiint(p) + (__double2loint(s) << 20), __double2loint(p));
 }
 
 constexpr int kSelBuf = 64;    // candidates that a wave ranks at a time: one per lane
 constexpr int kSelLists = 64;  // lists that a wave joins: one per lane
 
-// What a wave knows of its part of a row: the `beam` largest logits, in lanes 0 .. beam - 1 in order (of equal ones the smaller index
-// first; -inf behind the last), and sum exp(x - ref), each lane's share of it.
+// A logit and its index as one number: the larger comes first (the larger logit, of equal ones the smaller index).
+typedef unsigned long long cand_t;
+constexpr cand_t kNoCand = (cand_t)0x007fffffu << 32;  // -inf at index 0x7fffffff; below it: nothing
+__device__ __forceinline__ cand_t make_cand(float v, int i) { return (cand_t)orderable(v) << 32 | (uint32_t)(0x7fffffff - i); }
+__device__ __forceinline__ float cand_value(cand_t c) { return from_orderable((uint32_t)(c >> 32)); }
+__device__ __forceinline__ int cand_index(cand_t c) { return 0x7fffffff - (int)(uint32_t)c; }
+
+// What a wave knows of its part of a row: the `beam` best logits, in lanes 0 .. beam - 1 in order (kNoCand behind the last), and
+// sum exp(x - ref), each lane's share of it.
 struct RowPart {
-  float v = -INFINITY;
-  int i = 0x7fffffff;
+  cand_t best = kNoCand;
   double sum = 0.;
   float ref = -INFINITY;
   bool bad = false;  // a NaN or +inf among them (of this lane)
 };
 
-struct CandBuf {
-  float v[kSelBuf];
-  int i[kSelBuf];
+struct alignas(16) CandBuf {
+  cand_t c[kSelBuf];
 };
 
-// Lanes 0 .. n - 1 hold candidates: each one's rank among them goes to the list of the best `beam`.
-__device__ __forceinline__ void rank_candidates(float v, int i, int n, int beam, CandBuf &buf, float &out_v, int &out_i) {
+// The first n places of the buffer hold candidates: the best `beam` of them go to its first places in order, kNoCand behind the last.
+__device__ __forceinline__ cand_t rank_candidates(int n, int beam, CandBuf &buf) {
   const int lane = threadIdx.x & 63;
+  wave_lds_order();
+  if (lane >= n) buf.c[lane] = 0;
+  wave_lds_order();
+  const cand_t own = buf.c[lane];
   int rank = 0;
-  for (int j = 0; j < n; ++j) rank += comes_before_count(readlane_f(v, j), __builtin_amdgcn_readlane(i, j), v, i);
+  for (int j = 0; j < n; j += 8)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) rank += buf.c[j + u] > own;
   wave_lds_order();
-  if (lane < beam) {  // (places without a candidate come as equal ones, of which but one rank is filled)
-    buf.v[lane] = -INFINITY;
-    buf.i[lane] = 0x7fffffff;
-  }
+  if (lane < beam) buf.c[lane] = kNoCand;  // (equal ones, places without a candidate, have one rank)
   wave_lds_order();
-  if (lane < n && rank < beam) {
-    buf.v[rank] = v;
-    buf.i[rank] = i;
-  }
+  if (lane < n && rank < beam) buf.c[rank] = own;
   wave_lds_order();
-  out_v = lane < beam ? buf.v[lane] : -INFINITY;
-  out_i = lane < beam ? buf.i[lane] : 0x7fffffff;
+  const cand_t out = lane < beam ? buf.c[lane] : kNoCand;
   wave_lds_order();
+  return out;
 }
 
 // One tile of 64 * E logits of a row from index `base` on, lane l's in x: adds them to the sum and the list.
@@ -89,9 +96,9 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
   }
   const double ref = part.ref;
 #pragma unroll
-  for (int e = 0; e < E; ++e) part.sum += exp2_d(((double)x[e] - ref) * kLog2E);
+  for (int e = 0; e < E; ++e) part.sum += exp_d((double)x[e] - ref);
 
-  const float last = readlane_f(part.v, beam - 1);
+  const float last = readlane_f(cand_value(part.best), beam - 1);
   if (!(most > last)) return;  // equal ones come after those of the list, whose indices are smaller
   float bound = from_orderable(orderable(last) + 1);
   if (__popcll(__ballot(top > last)) >= beam) {
@@ -113,14 +120,11 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
     const uint64_t at = __ballot(in);
     if (at) {
       const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
-      if (in && pos < kSelBuf) {
-        buf.v[pos] = x[e];
-        buf.i[pos] = index(e);
-      }
+      if (in && pos < kSelBuf) buf.c[pos] = make_cand(x[e], index(e));
       n += __popcll(at);
     }
   }
-  const int held = __popcll(__ballot(lane < beam && part.v > -INFINITY));
+  const int held = __popcll(__ballot(lane < beam && part.best > kNoCand));
   if (n + held > kSelBuf) {
     uint32_t taken = 0;
     n = 0;
@@ -139,21 +143,13 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
       if (!(v > last)) break;
       if (own == i) taken |= 1u << at;
       wave_lds_order();
-      if (lane == 0) {
-        buf.v[n] = v;
-        buf.i[n] = i;
-      }
+      if (lane == 0) buf.c[n] = make_cand(v, i);
       ++n;
     }
   }
   wave_lds_order();
-  if (lane < held) {
-    buf.v[n + lane] = part.v;
-    buf.i[n + lane] = part.i;
-  }
-  n += held;
-  wave_lds_order();
-  rank_candidates(lane < n ? buf.v[lane] : -INFINITY, lane < n ? buf.i[lane] : 0x7fffffff, n, beam, buf, part.v, part.i);
+  if (lane < held) buf.c[n + lane] = part.best;
+  part.best = rank_candidates(n + held, beam, buf);
 }
 
 // A wave's part [begin, end) of a row.
@@ -200,8 +196,7 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 
 // A list as it is handed on: the best of a part of a row and the sum of its exponentials.
 struct SelList {
-  float v[kMaxBeam];
-  int i[kMaxBeam];
+  cand_t c[kMaxBeam];
 };
 struct SelStat {
   double sum;  // NaN: a NaN or +inf among the logits
@@ -241,10 +236,8 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
   const int l = min(lane, n_lists - 1), k = l / parts;
   // everything that is read leaves at once (what a finished hypothesis' lists hold is not looked at)
   const SelStat st = stats[l];
-  float v[kMaxBeam];
-  int i[kMaxBeam];
-  __builtin_memcpy(v, lists[l].v, sizeof(v));
-  __builtin_memcpy(i, lists[l].i, sizeof(i));
+  cand_t c[kMaxBeam];
+  __builtin_memcpy(c, lists[l].c, sizeof(c));
   const double score = a.scores[(int64_t)b * beam + k];
   const bool finished = a.done && a.done[(int64_t)b * beam + k];
   // log sum exp of the row
@@ -262,8 +255,12 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
   }
   const double lse = (double)ref + log(sum);
   double key[kMaxBeam];
+  float v[kMaxBeam];
+  int i[kMaxBeam];
 #pragma unroll
   for (int j = 0; j < kMaxBeam; ++j) {
+    v[j] = cand_value(c[j]);
+    i[j] = cand_index(c[j]);
     key[j] = score + ((double)v[j] - lse);
     if (!(key[j] == key[j] && v[j] > -INFINITY && j < beam) || finished || lane >= n_lists) key[j] = -INFINITY;
   }
@@ -342,10 +339,7 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
 
 __device__ __forceinline__ void put_list(const RowPart &part, double sum, bool bad, int beam, SelList &list, SelStat &stat) {
   const int lane = threadIdx.x & 63;
-  if (lane < beam) {
-    list.v[lane] = part.v;
-    list.i[lane] = part.i;
-  }
+  if (lane < beam) list.c[lane] = part.best;
   if (lane == 0) stat = SelStat{bad ? (double)NAN : sum, part.ref, 0};
 }
 
@@ -377,6 +371,7 @@ __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
 // that reach it and what earlier tiles left, rarely more than twice `beam`, one wave takes the best.
 struct SelScan {
   float group[32];
+  uint4 group_key[8];  // the same as whole numbers, made different by their number in the last bits: a little smaller, which a bound may be
   CandBuf buf;  // the list, in its first `beam` places, and what a tile adds
   int n;
   CandBuf wave_buf[4];
@@ -387,7 +382,7 @@ struct SelScan {
 template <typename TT, int E>
 __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
   typedef typename TT::T T;
-  constexpr int VE = 16 / sizeof(T), NV = E / VE, FOURS = E / 4;
+  constexpr int VE = 16 / sizeof(T), NV = E / VE;
   __shared__ SelScan sh;
   const int p = blockIdx.x % a.parts, row_i = blockIdx.x / a.parts, b = row_i / a.beam, k = row_i - b * a.beam, beam = a.beam;
   if (a.done && a.done[row_i]) return;  // (the join takes nothing from its lists)
@@ -398,10 +393,9 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
   double sum = 0.;
   float ref = -INFINITY, last = -INFINITY;  // of the block's list: its beam-th
   bool bad = false, many = false;
-  if (threadIdx.x < kSelBuf) {
-    sh.buf.v[threadIdx.x] = -INFINITY;
-    sh.buf.i[threadIdx.x] = 0x7fffffff;
-  }
+  int held = 0;  // places of the list that are filled
+  if (threadIdx.x < kMaxBeam) sh.buf.c[threadIdx.x] = kNoCand;
+  const int ranker = blockIdx.x / 256 & 3;  // of the blocks that share a unit each another wave, so another SIMD
   for (int base = begin; base < end; base += 256 * E) {
     float x[E];
     const int mine = base + wave * 64 * E + lane * VE;  // of vector i: 64 VE i further on
@@ -430,20 +424,59 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
         }
       }
     }
-    float four[FOURS];  // NaN if one of them is
+    float top = x[0];  // NaN if one of them is
 #pragma unroll
-    for (int e = 0; e < FOURS; ++e)
-      four[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[4 * e], x[4 * e + 1]), __builtin_elementwise_maximum(x[4 * e + 2], x[4 * e + 3]));
-    float top = four[0];
-#pragma unroll
-    for (int e = 1; e < FOURS; ++e) top = __builtin_elementwise_maximum(top, four[e]);
+    for (int e = 1; e < E; ++e) top = __builtin_elementwise_maximum(top, x[e]);
     bad |= !(top < INFINITY);
     const float eight = group_max<8>(top);
-    if ((lane & 7) == 0) sh.group[wave * 8 + (lane >> 3)] = eight;
+    if ((lane & 7) == 0) {
+      const int i = wave * 8 + (lane >> 3);
+      sh.group[i] = eight;
+      reinterpret_cast<uint32_t *>(sh.group_key)[i] = (orderable(eight) & ~31u) | i;
+    }
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    const float g = sh.group[lane & 31];
-    const float most = wave_max(g);
+    const float most = wave_max(sh.group[lane & 31]);
+    // (equal logits come after those of the list, whose indices are smaller)
+    if (!many && most > last) {
+      // (half a wave compares with half of the groups)
+      const uint32_t key = reinterpret_cast<const uint32_t *>(sh.group_key)[lane & 31];
+      int rank = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint4 o = sh.group_key[(lane >> 5) * 4 + j];
+        rank += (int)(o.x > key) + (int)(o.y > key) + (int)(o.z > key) + (int)(o.w > key);
+      }
+      rank += __shfl_xor(rank, 32);
+      const uint32_t nth = __builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(rank == beam - 1)) - 1) & ~31u;
+      const uint32_t after = orderable(last) + 1;
+      const float bound = from_orderable(nth > after ? nth : after);
+      // (a wave asks for all its places at once; most of its elements have no lane that reaches the bound)
+      uint64_t at[E];
+      int count = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        at[e] = __ballot(x[e] >= bound);
+        count += __popcll(at[e]);
+      }
+      if (count) {
+        int pos = 0;
+        if (lane == 0) pos = atomicAdd(&sh.n, count);
+        pos = held + __builtin_amdgcn_readfirstlane(pos);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (at[e]) {
+            const int to = pos + __builtin_amdgcn_mbcnt_hi((uint32_t)(at[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at[e], 0));
+            if (x[e] >= bound && to < kSelBuf) sh.buf.c[to] = make_cand(x[e], mine + (e / VE) * 64 * VE + e % VE);
+            pos += __popcll(at[e]);
+          }
+      }
+    }
+    __syncthreads();
+    const int n = sh.n;
+    many = many || held + n > kSelBuf;
+    // one wave ranks while the others add up
+    if (n && !many && wave == ranker) rank_candidates(held + n, beam, sh.buf);
     if (most > -INFINITY) {
       if (!(most < ref + 500.f)) {  // (the first tile too; float64 holds exp(500) times exp(200) more)
         const float to = most < INFINITY ? most : 0.f;
@@ -452,47 +485,13 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
       }
       const double r = ref;
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum += exp2_d(((double)x[e] - r) * kLog2E);
+      for (int e = 0; e < E; ++e) sum += exp_d((double)x[e] - r);
     }
-    // (equal logits come after those of the list, whose indices are smaller)
-    if (!many && most > last) {
-      // (the groups' maxima made different by their number in the last bits: a little smaller, which a bound may be)
-      const uint32_t key = (orderable(g) & ~31u) | (lane & 31);
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < 32; ++j) rank += (uint32_t)__builtin_amdgcn_readlane((int)key, j) > key;
-      const uint32_t nth = __builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(rank == beam - 1)) - 1) & ~31u;
-      const uint32_t after = orderable(last) + 1;
-      const float bound = from_orderable(nth > after ? nth : after);
-#pragma unroll
-      for (int f = 0; f < FOURS; ++f) {
-        if (!__any(four[f] >= bound)) continue;
-#pragma unroll
-        for (int e = 4 * f; e < 4 * f + 4; ++e)
-          if (x[e] >= bound) {
-            const int pos = beam + atomicAdd(&sh.n, 1);
-            if (pos < kSelBuf) {
-              sh.buf.v[pos] = x[e];
-              sh.buf.i[pos] = mine + (e / VE) * 64 * VE + e % VE;
-            }
-          }
-      }
-    }
+    if (base + 256 * E >= end) break;
     __syncthreads();
-    const int n = sh.n;
-    if (n) {
-      many = many || beam + n > kSelBuf;
-      if (!many && wave == 0) {
-        const bool in = lane < beam + n;
-        float v = in ? sh.buf.v[lane] : -INFINITY;
-        int i = in ? sh.buf.i[lane] : 0x7fffffff;
-        rank_candidates(v, i, beam + n, beam, sh.buf, v, i);
-      }
-      __syncthreads();
-      last = sh.buf.v[beam - 1];
-    }
+    if (n) held = beam;
+    last = cand_value(sh.buf.c[beam - 1]);
   }
-  if (lane == 0) sh.stat[wave].sum = 0.;
   sum = wave_sum_d(sum);
   if (lane == 0) sh.stat[wave].sum = __any(bad) ? (double)NAN : sum;
   if (many) {
@@ -505,18 +504,13 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
     __syncthreads();
     if (wave == 0) {
       const int w = lane / beam, e = lane - w * beam;
-      const bool in = lane < 4 * beam;
-      float v = in ? sh.list[w].v[e] : -INFINITY;
-      int i = in ? sh.list[w].i[e] : 0x7fffffff;
-      rank_candidates(v, i, 4 * beam, beam, sh.buf, v, i);
+      if (lane < 4 * beam) sh.buf.c[lane] = sh.list[w].c[e];
+      rank_candidates(4 * beam, beam, sh.buf);
     }
   }
   __syncthreads();
   if (wave) return;
-  if (lane < beam) {
-    a.lists[at].v[lane] = sh.buf.v[lane];
-    a.lists[at].i[lane] = sh.buf.i[lane];
-  }
+  if (lane < beam) a.lists[at].c[lane] = sh.buf.c[lane];
   if (lane == 0) a.stats[at] = SelStat{(sh.stat[0].sum + sh.stat[1].sum) + (sh.stat[2].sum + sh.stat[3].sum), ref, 0};
 }
 
