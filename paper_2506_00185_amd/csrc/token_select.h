@@ -46,8 +46,29 @@ struct RowPart {
   bool bad = false;  // a NaN or +inf among them (of this lane)
 };
 
+// The maxima of 32 groups of logits as whole numbers, made different by their group's number in the last bits: a little smaller, which
+// a bound may be.
+struct alignas(16) GroupKeys {
+  uint32_t k[32];
+};
+__device__ __forceinline__ uint32_t group_key(float v, int group) { return (orderable(v) & ~31u) | group; }
+// what the `nth` (1 ..) largest of them reaches, as orderable() has it
+__device__ __forceinline__ uint32_t nth_group(const GroupKeys &g, int nth) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t key = g.k[lane & 31];
+  int rank = 0;  // half a wave compares with half of the groups
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint4 o = reinterpret_cast<const uint4 *>(g.k)[(lane >> 5) * 4 + j];
+    rank += (int)(o.x > key) + (int)(o.y > key) + (int)(o.z > key) + (int)(o.w > key);
+  }
+  rank += __shfl_xor(rank, 32);
+  return __builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(rank == nth - 1)) - 1) & ~31u;
+}
+
 struct alignas(16) CandBuf {
   cand_t c[kSelBuf];
+  GroupKeys group;
 };
 
 // The first n places of the buffer hold candidates: the best `beam` of them go to its first places in order, kNoCand behind the last.
@@ -72,7 +93,7 @@ __device__ __forceinline__ cand_t rank_candidates(int n, int beam, CandBuf &buf)
 }
 
 // One tile of 64 * E logits of a row from index `base` on, lane l's in x: adds them to the sum and the list.
-// The list: a bound that the `beam` best reach is the beam-th largest of the lanes' maxima, or what the list holds already; those logits that
+// The list: a bound that the `beam` best reach is the beam-th largest of the maxima of 32 pairs of lanes, or what the list holds already; those logits that
 // reach it, few more than `beam` as a rule, are collected and ranked.  Where more than a wave ranks at a time reach it (many equal
 // logits), the best are taken out one after the other instead.
 template <int E, int VE>
@@ -100,27 +121,19 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
 
   const float last = readlane_f(cand_value(part.best), beam - 1);
   if (!(most > last)) return;  // equal ones come after those of the list, whose indices are smaller
-  float bound = from_orderable(orderable(last) + 1);
-  if (__popcll(__ballot(top > last)) >= beam) {
-    float rest = top, m = most;
-    int n = 0;
-    while (true) {
-      const uint64_t at = __ballot(rest == m);
-      n += __popcll(at);
-      if (n >= beam) break;
-      rest = rest == m ? -INFINITY : rest;
-      m = wave_max(rest);
-    }
-    bound = m;
-  }
+  const float pair = fmaxf(top, dpp_f<kDppXor1>(top));
+  wave_lds_order();
+  if (!(lane & 1)) buf.group.k[lane >> 1] = group_key(pair, lane >> 1);
+  wave_lds_order();
+  const uint32_t nth = nth_group(buf.group, beam), after = orderable(last) + 1;
+  const float bound = from_orderable(nth > after ? nth : after);
   int n = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const bool in = x[e] >= bound;
-    const uint64_t at = __ballot(in);
+    const uint64_t at = __ballot(x[e] >= bound);
     if (at) {
       const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
-      if (in && pos < kSelBuf) buf.c[pos] = make_cand(x[e], index(e));
+      if (x[e] >= bound && pos < kSelBuf) buf.c[pos] = make_cand(x[e], index(e));
       n += __popcll(at);
     }
   }
@@ -217,15 +230,14 @@ struct SelectArgs {
   int B, beam, V, eos, parts, part_len;
 };
 
-struct SelJoin {
-  double key[kSelLists][kMaxBeam + 1];  // of the lists' candidates
-  double cand_key[kSelLists * kMaxBeam];
-  int cand_at[kSelLists * kMaxBeam];
-  float cand_x[kSelLists * kMaxBeam];  // their logits
-  uint8_t cand_k[kSelLists * kMaxBeam];
+struct alignas(16) SelJoin {
+  float low[64];  // the first few of every list, rounded down
+  double key[kSelLists * kMaxBeam];  // of the candidates
+  int token[kSelLists * kMaxBeam];
+  float x[kSelLists * kMaxBeam];
+  uint8_t k[kSelLists * kMaxBeam];
   double sum[kSelLists];
   float ref[kSelLists];
-  int n;
 };
 
 // One wave: the `beam` best of an utterance from the lists of its rows, lane l's being list l = k * parts + p.  A bound that they reach is the
@@ -254,80 +266,62 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     for (int p = 0; p < parts; ++p) sum += sh.sum[k * parts + p];
   }
   const double lse = (double)ref + log(sum);
-  double key[kMaxBeam];
-  float v[kMaxBeam];
-  int i[kMaxBeam];
+  if (finished) c[0] = lane == k * parts ? make_cand(0.f, a.eos) : kNoCand;  // its one candidate: eos, with the score that it has
+  // (a list's keys descend; NaN is none)
+  const auto key_of = [&](int j) {
+    const double key = finished ? score : score + ((double)cand_value(c[j]) - lse);
+    return c[j] > kNoCand && key > -INFINITY && (j == 0 || !finished) && lane < n_lists ? key : -INFINITY;
+  };
+  // the bound, in float32 rounded down
+  const int firsts = max(min(64, 4 * beam) / n_lists, 1);
+  sh.low[lane] = -INFINITY;
+  wave_lds_order();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float one = (float)key_of(j);
+    if (j < firsts && lane < n_lists && one > -INFINITY) sh.low[lane * firsts + j] = from_orderable(orderable(one) - 1);  // (-inf for what float32 has no number for)
+  }
+  wave_lds_order();
+  const float low = sh.low[lane];
+  int before = 0;
+  for (int j = 0; j < n_lists * firsts; j += 8)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) before += sh.low[j + u] > low;
+  const double bound = -wave_max(before < beam ? -low : -INFINITY);
+  int n = 0;
 #pragma unroll
   for (int j = 0; j < kMaxBeam; ++j) {
-    v[j] = cand_value(c[j]);
-    i[j] = cand_index(c[j]);
-    key[j] = score + ((double)v[j] - lse);
-    if (!(key[j] == key[j] && v[j] > -INFINITY && j < beam) || finished || lane >= n_lists) key[j] = -INFINITY;
-  }
-  if (finished && lane == k * parts) {  // its one candidate: eos, with the score that it has
-    key[0] = score == score ? score : -INFINITY;
-    i[0] = a.eos;
-    v[0] = 0.f;
-  }
-#pragma unroll
-  for (int j = 0; j < kMaxBeam; ++j) sh.key[lane][j] = key[j];
-  if (lane == 0) sh.n = 0;
-  wave_lds_order();
-  // the bound, in float32 rounded down
-  const int firsts = max(min(64, 4 * beam) / n_lists, 1), list = lane / firsts;
-  const double one = list < n_lists ? sh.key[list][lane - list * firsts] : -INFINITY;
-  const float low = (float)one > -INFINITY ? from_orderable(orderable((float)one) - 1) : -INFINITY;  // (-inf for what float32 has no number for)
-  int before = 0;
-#pragma unroll 8
-  for (int j = 0; j < n_lists * firsts; ++j) before += readlane_f(low, j) > low;
-  const float bound = -wave_max(before < beam ? -low : -INFINITY);
-  int mine = 0;
-#pragma unroll
-  for (int j = 0; j < kMaxBeam; ++j) mine += key[j] > -INFINITY && key[j] >= (double)bound;  // (a list's keys descend)
-  if (mine) {
-    const int pos = atomicAdd(&sh.n, mine);
-#pragma unroll
-    for (int j = 0; j < kMaxBeam; ++j)
-      if (j < mine) {
-        sh.cand_key[pos + j] = key[j];
-        sh.cand_at[pos + j] = k * a.V + i[j];
-        sh.cand_x[pos + j] = v[j];
-        sh.cand_k[pos + j] = (uint8_t)k;
-      }
+    const double key = j < beam ? key_of(j) : -INFINITY;
+    const bool in = key > -INFINITY && key >= bound;
+    const uint64_t at = __ballot(in);
+    if (!at) break;
+    if (in) {
+      const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
+      sh.key[pos] = key;
+      sh.token[pos] = cand_index(c[j]);
+      sh.x[pos] = cand_value(c[j]);
+      sh.k[pos] = (uint8_t)k;
+    }
+    n += __popcll(at);
   }
   wave_lds_order();
-  const int n = sh.n;
   const int64_t out = (int64_t)b * beam;
-  auto put = [&](int r, double key, int flat) {
-    const int parent = flat / a.V, token = flat - parent * a.V;
+  for (int p = lane; p < n; p += 64) {
+    const double key = sh.key[p];
+    const float x = sh.x[p];
+    const int token = sh.token[p], parent = sh.k[p];
+    int r = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const double other = sh.key[j];
+      r += other > key;
+      if (other == key && j != p) r += sh.k[j] != parent ? sh.k[j] < parent : sh.x[j] != x ? sh.x[j] > x : sh.token[j] < token;
+    }
+    if (r >= beam) continue;
     a.out_scores[out + r] = key;
     a.out_parent[out + r] = parent;
     a.out_token[out + r] = token;
     if (a.out_done) a.out_done[out + r] = token == a.eos;
-  };
-  const auto first_of_equals = [](int k1, float x1, int flat1, int k2, float x2, int flat2) { return k1 == k2 && x1 != x2 ? x1 > x2 : flat1 < flat2; };
-  if (n <= 64) {
-    const double key = lane < n ? sh.cand_key[lane] : -INFINITY;
-    const int flat = lane < n ? sh.cand_at[lane] : 0x7fffffff, row = lane < n ? sh.cand_k[lane] : -1;
-    const float x = lane < n ? sh.cand_x[lane] : 0.f;
-    int r = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
-      const double other = readlane_d(key, j);
-      r += other > key;
-      if (__popcll(__ballot(other == key)) > 1)
-        r += other == key && first_of_equals(__builtin_amdgcn_readlane(row, j), readlane_f(x, j), __builtin_amdgcn_readlane(flat, j), row, x, flat);
-    }
-    if (lane < n && r < beam) put(r, key, flat);
-  } else {
-    for (int c = lane; c < n; c += 64) {
-      const double key = sh.cand_key[c];
-      int r = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j)
-        r += sh.cand_key[j] > key || (sh.cand_key[j] == key && first_of_equals(sh.cand_k[j], sh.cand_x[j], sh.cand_at[j], sh.cand_k[c], sh.cand_x[c], sh.cand_at[c]));
-      if (r < beam) put(r, key, sh.cand_at[c]);
-    }
   }
   for (int r = n + lane; r < beam; r += 64) {  // empty slots
     a.out_scores[out + r] = -INFINITY;
@@ -371,7 +365,7 @@ __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
 // that reach it and what earlier tiles left, rarely more than twice `beam`, one wave takes the best.
 struct SelScan {
   float group[32];
-  uint4 group_key[8];  // the same as whole numbers, made different by their number in the last bits: a little smaller, which a bound may be
+  GroupKeys group_key;
   CandBuf buf;  // the list, in its first `beam` places, and what a tile adds
   int n;
   CandBuf wave_buf[4];
@@ -432,24 +426,14 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
     if ((lane & 7) == 0) {
       const int i = wave * 8 + (lane >> 3);
       sh.group[i] = eight;
-      reinterpret_cast<uint32_t *>(sh.group_key)[i] = (orderable(eight) & ~31u) | i;
+      sh.group_key.k[i] = group_key(eight, i);
     }
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
     const float most = wave_max(sh.group[lane & 31]);
     // (equal logits come after those of the list, whose indices are smaller)
     if (!many && most > last) {
-      // (half a wave compares with half of the groups)
-      const uint32_t key = reinterpret_cast<const uint32_t *>(sh.group_key)[lane & 31];
-      int rank = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 o = sh.group_key[(lane >> 5) * 4 + j];
-        rank += (int)(o.x > key) + (int)(o.y > key) + (int)(o.z > key) + (int)(o.w > key);
-      }
-      rank += __shfl_xor(rank, 32);
-      const uint32_t nth = __builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(rank == beam - 1)) - 1) & ~31u;
-      const uint32_t after = orderable(last) + 1;
+      const uint32_t nth = nth_group(sh.group_key, beam), after = orderable(last) + 1;
       const float bound = from_orderable(nth > after ? nth : after);
       // (a wave asks for all its places at once; most of its elements have no lane that reaches the bound)
       uint64_t at[E];
