@@ -128,8 +128,9 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     raw, scope = _enter(T, logits, stream, (logits, scores, done) + tuple(out or ()))
     try:
         if out is None:
-            out = (T.empty_like(scores), T.empty(shape, dtype=T.i32, device=dev), T.empty(shape, dtype=T.i32, device=dev),
-                   T.empty(shape, dtype=T.bool, device=dev) if eos >= 0 else None)
+            whole = T.empty(shape, dtype=T.i32, device=dev)
+            out = (T.empty_like(scores), whole, T.empty_like(whole),
+                   None if eos < 0 else T.empty(shape, dtype=T.bool, device=dev) if done is None else T.empty_like(done))
             s.out_scores, s.out_parent, s.out_token = out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr()
         else:
             _refuse(len(out) == 4, "out must be (scores, parents, tokens, done)")
@@ -282,7 +283,8 @@ class KVCache:
         raw, scope = _enter(T, self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp))
         try:
             heads, dim = self.heads, self.dim
-            out = tuple(T.empty((B, n, heads, dim), dtype=dtype, device=self.device) for _ in range(2))
+            k = T.empty((B, n, heads, dim), dtype=dtype, device=self.device)
+            out = (k, T.empty_like(k))
             if n:
                 rk, rv = (_Rows(t.data_ptr(), n * heads * dim, heads * dim, dim) for t in out)
                 _check(T.lib.rnnt_cache_read(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
