@@ -374,7 +374,7 @@ struct SelScan {
 };
 
 template <typename TT, int E>
-__global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
+__global__ __launch_bounds__(256, 5) void k_select_scan(SelectArgs a) {
   typedef typename TT::T T;
   constexpr int VE = 16 / sizeof(T), NV = E / VE;
   __shared__ SelScan sh;
@@ -436,24 +436,23 @@ __global__ __launch_bounds__(256) void k_select_scan(SelectArgs a) {
       const uint32_t nth = nth_group(sh.group_key, beam), after = orderable(last) + 1;
       const float bound = from_orderable(nth > after ? nth : after);
       // (a wave asks for all its places at once; most of its elements have no lane that reaches the bound)
-      uint64_t at[E];
       int count = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        at[e] = __ballot(x[e] >= bound);
-        count += __popcll(at[e]);
-      }
+      for (int e = 0; e < E; ++e) count += __popcll(__ballot(x[e] >= bound));
       if (count) {
         int pos = 0;
         if (lane == 0) pos = atomicAdd(&sh.n, count);
         pos = held + __builtin_amdgcn_readfirstlane(pos);
+        float again = bound;
+        asm volatile("" : "+v"(again));  // (compared again: kept, the masks would not fit the scalar registers)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (at[e]) {
-            const int to = pos + __builtin_amdgcn_mbcnt_hi((uint32_t)(at[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at[e], 0));
-            if (x[e] >= bound && to < kSelBuf) sh.buf.c[to] = make_cand(x[e], mine + (e / VE) * 64 * VE + e % VE);
-            pos += __popcll(at[e]);
-          }
+        for (int e = 0; e < E; ++e) {
+          const uint64_t at = __ballot(x[e] >= again);
+          if (!at) continue;
+          const int to = pos + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
+          if (x[e] >= again && to < kSelBuf) sh.buf.c[to] = make_cand(x[e], mine + (e / VE) * 64 * VE + e % VE);
+          pos += __popcll(at);
+        }
       }
     }
     __syncthreads();
