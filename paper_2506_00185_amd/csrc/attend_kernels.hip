@@ -10,7 +10,10 @@ namespace rb {
 template <typename TT, int FMT>
 int launch_attend(const AttendArgs &a, int dp, int mt, int64_t blocks, hipStream_t stream) {
   int rc;
-  if (dp == 64) rc = launch(mt == 1 ? k_attend<TT, FMT, 64, 1> : k_attend<TT, FMT, 64, 2>, blocks, 1, 256, a, stream);
+  if (dp == 64) {
+    if constexpr (FMT == 16) rc = launch(mt == 1 ? k_attend<TT, FMT, 64, 1> : k_attend<TT, FMT, 64, 2>, blocks, 1, 256, a, stream);
+    else rc = launch(k_attend<TT, FMT, 64, 1>, blocks, 1, 256, a, stream);
+  }
   else if (dp == 128) rc = launch(mt == 1 ? k_attend<TT, FMT, 128, 1> : k_attend<TT, FMT, 128, 2>, blocks, 1, 256, a, stream);
   else rc = launch(k_attend<TT, FMT, 256, 1>, blocks, 1, 256, a, stream);
   if (rc || a.splits == 1) return rc;

@@ -40,14 +40,11 @@ int cache_view(const rnnt_cache_t *c, CacheView &v) {
 
 template <typename TT, int FMT, bool WRITE, int LANES>
 int rows_lanes(RowsArgs &a, hipStream_t stream) {
-  constexpr int kRows = 256 / LANES;
-  const int rows = a.n * a.c.heads;
-  // four rows for a group of lanes where that leaves two blocks for every unit: loads of a block under way; else one, for more blocks
-  const bool four = (int64_t)a.B * ((rows + 4 * kRows - 1) / (4 * kRows)) * 2 >= 2 * kUnits;
-  a.blocks = (rows + kRows * (four ? 4 : 1) - 1) / (kRows * (four ? 4 : 1));
+  constexpr int kRows = kRowsOfGroup * 256 / LANES;
+  a.blocks = (a.n * a.c.heads + kRows - 1) / kRows;
   const int64_t blocks = (int64_t)a.B * a.blocks;
-  if constexpr (WRITE) return launch(four ? k_cache_write<TT, FMT, LANES, 4> : k_cache_write<TT, FMT, LANES, 1>, blocks, 2, 256, a, stream);
-  else return launch(four ? k_cache_read<TT, FMT, LANES, 4> : k_cache_read<TT, FMT, LANES, 1>, blocks, 2, 256, a, stream);
+  if constexpr (WRITE) return launch(k_cache_write<TT, FMT, LANES>, blocks, 2, 256, a, stream);
+  else return launch(k_cache_read<TT, FMT, LANES>, blocks, 2, 256, a, stream);
 }
 template <typename TT, int FMT, bool WRITE>
 int rows_typed(RowsArgs &a, hipStream_t stream) {
@@ -96,7 +93,7 @@ int rows_call(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t
   return refuse("unknown type");
 }
 
-// How the work of a call is cut: see attend_plan
+// How the work of a call is cut
 struct AttendPlan {
   int dp, mt, rows, row_tiles, splits, split_len, join_shares;
   int64_t blocks, workspace;
@@ -111,11 +108,18 @@ int attend_plan(const CacheView &c, bool f8, const rnnt_attend_t *s, AttendPlan 
   if (rows > 1 << 24 || pairs > 1 << 24 || rows * pairs > (int64_t)1 << 32) return refuse("more work than one launch takes");
   p.rows = (int)rows;
   p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-  p.mt = rows > 16 && p.dp < 256 ? 2 : 1;
+  // Two tiles of rows for a block: a token's key and value are loaded and unpacked once for both, but half as many waves fit.  That pays where
+  // blocks of one tile would fill the chip, and where a row is more than 64 bytes (trees of 61 nodes over 500 to 2000 tokens, microseconds with
+  // one tile and two: 16 sequences x 32 heads on 8 of 128, float32 on a cache of 16 bits 133 and 88, bfloat16 on e4m3 84 and 64; of 64 on 16
+  // bits 75 and 55, on e4m3 46 and 44, but 24 and 24 with 8 sequences x 16 heads, and 57 and 67 for 2 chunks of 2000; 2 sequences x 8 heads of 128: 20 and 23).
+  // With 256 dims the sums of two tiles do not fit the registers.
+  const int64_t tiles = (rows + 15) / 16;
+  p.mt = tiles > 1 && pairs * tiles > kUnits && (f8 ? p.dp == 128 : p.dp < 256) ? 2 : 1;
   p.row_tiles = (int)((rows + 16 * p.mt - 1) / (16 * p.mt));
   // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for two on every unit, four where a
-  // unit holds three, none shorter
-  // than 256 tokens, two tiles for each of its waves
+  // unit holds three or more (32 sequences of 1000 to 8000 tokens, 32 heads on 8 of 128: 75 us with two, 65 with four, 70 with six; where it holds two, four
+  // cost: 16 trees of 61 nodes 64 us for 51), none shorter than 256 tokens, two tiles for each of its waves (one sequence of 8000 tokens:
+  // 15.7 us from 128 tokens on, 12.7 from 256, 14.2 from 512).
   const int64_t room = (int64_t)c.width << c.page_shift, longest = s->max_len < room ? (s->max_len > 1 ? s->max_len : 1) : room;
   const int64_t others = pairs * p.row_tiles, want = ((attend_blocks(f8 ? 8 : 16, p.dp, p.mt) > 2 ? 4 : 2) * kUnits + others - 1) / others, most = (longest + 255) / 256;
   int64_t splits = want < most ? want : most;
@@ -124,7 +128,7 @@ int attend_plan(const CacheView &c, bool f8, const rnnt_attend_t *s, AttendPlan 
   p.splits = (int)splits;
   p.split_len = (int)len;
   p.blocks = (pairs * splits + 7) / 8 * 8 * p.row_tiles;
-  p.join_shares = 1;  // four splits for each thread of the join
+  p.join_shares = 1;  // four splits for each thread of the join (one sequence of 8000 tokens: 12.7 us, with all splits on one thread 15.6)
   while (p.join_shares < 8 && p.join_shares * 4 < splits && c.dim / 4 * p.join_shares * 2 <= 256) p.join_shares *= 2;
   p.workspace = splits > 1 ? splits * pairs * rows * (int64_t)(c.dim * sizeof(float) + sizeof(float2)) : 0;
   return RNNT_OK;

@@ -302,6 +302,21 @@ def test_trees_and_chunks(fmt, dtype, dim, heads, group, n):
     check(cache, table, q[:, :1], lens, some_tree(g, 4, n, padded=False), dtype=dtype)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,heads,group,n", [(64, 5, 4, 30), (80, 3, 5, 37), (128, 4, 3, 43)])
+def test_trees_and_chunks_of_many_rows(fmt, dtype, dim, heads, group, n):
+    """Enough rows for blocks of two tiles; the last tile and its second half filled in part."""
+    g = np.random.default_rng(dim + n)
+    lens = np.array([0, 5, 64, 130, 31, 32, 33, 0, 97, 128])
+    cache, table = filled(g, len(lens), 130 + n, heads, dim, fmt, 16)
+    q = cuda(g.standard_normal((len(lens), n, heads * group, dim)), R.torch_type(dtype))
+    assert len(lens) * heads * -(-n * group // 16) > 256
+    check(cache, table, q, lens, some_tree(g, len(lens), n), dtype=dtype)
+    check(cache, table, q, lens, dtype=dtype)
+    check(cache, table, q, lens - 3, some_tree(g, len(lens), n + 3, padded=False), dtype=dtype)
+
+
 @pytest.mark.parametrize("length,n,B", [(2500, 1, 1), (5000, 3, 2), (40, 300, 1), (1000, 70, 2), (9000, 1, 3)])
 def test_lengths_that_are_split(length, n, B):
     g = np.random.default_rng(length)
