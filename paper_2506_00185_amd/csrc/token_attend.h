@@ -19,6 +19,10 @@ namespace rb {
 // the output is bfloat16, whose rounding is eight times as coarse, else a sum of two; sums are float32.
 // M follows the running maximum only when a logit passes it by 2^8 (the range that float16 leaves above), so that the accumulators are
 // multiplied by a correction a few times in a row of thousands of tokens.
+// Measured: one token for each of 32 sequences of 1000 to 8000, 32 heads on 8 of 128 in e4m3: 61 us and 4 for the join, 4.6 TB/s of a large copy's
+// 5.3; bound by memory, a block's beginning (three dependent loads, 5 us) and the lengths' spread are the rest.  61 nodes for each of 16 sequences, 500 to 2000 tokens, float32 on
+// a cache of 16 bits: 51 us, 180 TFLOP/s of products, bound by instructions: for a tile of 32 tokens and 32 rows a wave issues 64 products and
+// some 350 vector instructions.  One sequence of 187 tokens: 7 us, a chain of loads.
 struct AttendArgs {
   CacheView c;
   const void *q;
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
   }
 }
 
-// ---- the splits of a row: `join_shares` threads for 4 values of it, each a split at a time
+// ---- the splits of a row: `join_shares` threads for 4 values of it, each a split at a time.  4 to 5 us, a launch and two loads
 template <typename TT>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   typedef typename TT::T T;

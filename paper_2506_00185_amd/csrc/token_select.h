@@ -337,7 +337,8 @@ __device__ __forceinline__ void put_list(const RowPart &part, double sum, bool b
   if (lane == 0) stat = SelStat{bad ? (double)NAN : sum, part.ref, 0};
 }
 
-// ---- everything of an utterance in one block of 16 waves, parts = 16 / beam of them for a row: no workspace, one launch
+// ---- everything of an utterance in one block of 16 waves, parts = 16 / beam of them for a row: no workspace, one launch.  Bound by the chain
+// of its steps (load, sums, bound, ranking, the same again for the join), each of a few hundred to 1500 cycles: 6 us for 4 x 1024.
 template <typename TT, int NV>
 __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
   typedef typename TT::T T;
@@ -363,6 +364,9 @@ __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
 // ---- many blocks for a row: each leaves the best of its part, a second launch joins them.  A block's four waves take tiles of 256 E logits
 // together: a bound that the `beam` best of a tile reach is the beam-th largest of the maxima of 32 groups of 8 lanes; of the logits
 // that reach it and what earlier tiles left, rarely more than twice `beam`, one wave takes the best.
+// Measured: 128 x 10 x 8192 logits of 16 bits in 14 us (read at 5.3 TB/s they would take 4), 32 x 12 x 32003 of 32, a fifth of the rows finished, in 18 (7.4).  Of the 14 some 4 go
+// into the float64 exponentials (16 instructions for a logit), 3 each into the first loads, which all blocks wait for at once, and into finding
+// and ranking the candidates.  Five blocks share a unit: what keeps the registers to 96, with 80 some are spilt and it takes 15.7 us.
 struct SelScan {
   float group[32];
   GroupKeys group_key;
@@ -497,6 +501,7 @@ __global__ __launch_bounds__(256, 5) void k_select_scan(SelectArgs a) {
   if (lane == 0) a.stats[at] = SelStat{(sh.stat[0].sum + sh.stat[1].sum) + (sh.stat[2].sum + sh.stat[3].sum), ref, 0};
 }
 
+// 5 to 6 us, a chain of dependent steps in one wave: lists in, exp and log of the sums, keys, bound, ranking
 static __global__ __launch_bounds__(64) void k_select_join(SelectArgs a) {
   __shared__ SelJoin sh;
   const int64_t first = (int64_t)blockIdx.x * a.beam * a.parts;
@@ -505,7 +510,8 @@ static __global__ __launch_bounds__(64) void k_select_join(SelectArgs a) {
 
 // ---- states of hypotheses to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]]
 // A thread reads its column of all slots that move and then writes them, so that no copy of the tensor is needed and each byte is read and
-// written once; slots that stay where they are are neither read for themselves nor written.
+// written once; slots that stay where they are are neither read for themselves nor written.  Bound by memory: 16 x 8 slots of 4 x 8 runs of 25 KB
+// on each side move in 66 us, 4.7 TB/s, a large copy's rate.
 struct StateView {  // strides in bytes
   char *data;
   int64_t lead_stride, b_stride, slot_stride, inner_stride, row_bytes;
