@@ -2,7 +2,8 @@
 rnnt_cache_write / read / attend and rnnt_nbest_tree.  Argument checks and marshalling only; include/rnnt_beam.h says what each does.
 
 Tensors live on one GPU; work goes to ``stream`` (default: the current stream of that GPU) and the calls return without
-waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph."""
+waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph.  The calls are for
+inference: a tensor that requires a gradient is refused."""
 from __future__ import annotations
 
 import contextlib
@@ -55,6 +56,7 @@ class _Torch:
         import torch
         self.empty, self.empty_like, self.device_of = torch.empty, torch.empty_like, torch.cuda.current_device
         self.f64, self.f32, self.i32, self.u8, self.bool = torch.float64, torch.float32, torch.int32, torch.uint8, torch.bool
+        self.grads = torch.is_grad_enabled
         self.types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         # (the pointer alone where this torch gives it without an object around it)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -75,6 +77,8 @@ def _type_of(T, t, what):
     code = T.types.get(t.dtype)
     if code is None:
         raise RnntBeamError(f"{what} must be float32, float16 or bfloat16")
+    if t.requires_grad and T.grads():
+        raise RnntBeamError(f"{what} requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
     return code
 
 
@@ -262,6 +266,7 @@ class KVCache:
             raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
         B, n = shape[0], shape[1]
         code, c = _type_of(T, k, "k"), self._view(T, table, B)
+        _type_of(T, v, "v")
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))

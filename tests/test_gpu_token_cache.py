@@ -208,6 +208,10 @@ def test_what_the_cache_refuses():
                   ((q, table, start), dict(parents=cuda(np.zeros((3, 1025), np.int32)))), ((q[:, :0], table, start), {})]:
         with pytest.raises(RnntBeamError):
             c.attend(*a, **kw)
+    leaf = k.clone().requires_grad_()
+    for call in (lambda: c.write(leaf, k, table, start), lambda: c.write(k, leaf, table, start), lambda: c.attend(q.clone().requires_grad_(), table, start)):
+        with pytest.raises(RnntBeamError, match="gradient"):
+            call()
     for bad in [(0, 16, 2, 64), (4, 12, 2, 64), (4, 16, 2, 40)]:
         with pytest.raises(RnntBeamError):
             cache = KVCache(*bad)

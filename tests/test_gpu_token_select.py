@@ -178,6 +178,23 @@ def test_scores_that_float32_does_not_hold(V):
     assert got[2][0].tolist() == logits[0, 0].topk(4).indices.tolist()
 
 
+def test_the_longest_row():
+    """Indices up to the last that is allowed; equal logits everywhere else."""
+    import math
+    import torch
+    V = 2**31 - 2**16
+    logits = torch.zeros(1, 1, V, dtype=torch.bfloat16, device="cuda")
+    for at in (V - 1, V // 2 + 1, 0):
+        logits[0, 0, at] = 12.0
+        got = run(logits, np.array([[-3.0]]))
+        logits[0, 0, at] = 0.0
+        assert got[1][0, 0] == 0 and got[2][0, 0] == at
+        # (a lane adds V / 64 / 256 terms, less than 2^17, each sum off by up to half a step)
+        assert abs(got[0][0, 0] - (9.0 - math.log(V - 1 + math.exp(12.0)))) <= KEY_ATOL + (2**17 + 64) * 2.0**-53
+    del logits
+    torch.cuda.empty_cache()
+
+
 def test_in_place_and_on_another_stream():
     import torch
     from paper_2506_00185_amd import select_tokens
@@ -239,6 +256,10 @@ def test_what_python_refuses():
     for args in bad:
         with pytest.raises(RnntBeamError):
             select_tokens(*args)
+    with pytest.raises(RnntBeamError, match="gradient"):
+        select_tokens(x.clone().requires_grad_(), s)
+    with torch.no_grad():
+        select_tokens(x.clone().requires_grad_(), s)
     with pytest.raises(RnntBeamError, match="beam"):
         select_tokens(torch.zeros(1, 17, 5, device="cuda"), torch.zeros(1, 17, dtype=torch.float64, device="cuda"))
     with pytest.raises(RnntBeamError):
