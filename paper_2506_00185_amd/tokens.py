@@ -54,7 +54,9 @@ class _Torch:
 
     def __init__(self):
         import torch
-        self.empty, self.empty_like, self.device_of = torch.empty, torch.empty_like, torch.cuda.current_device
+        # (of equals the faster one: a tensor like another, the device's number without a check that there is a device)
+        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.device_of = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.f64, self.f32, self.i32, self.u8, self.bool = torch.float64, torch.float32, torch.int32, torch.uint8, torch.bool
         self.grads = torch.is_grad_enabled
         self.types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -132,9 +134,8 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     raw, scope = _enter(T, logits, stream, (logits, scores, done) + tuple(out or ()))
     try:
         if out is None:
-            whole = T.empty(shape, dtype=T.i32, device=dev)
-            out = (T.empty_like(scores), whole, T.empty_like(whole),
-                   None if eos < 0 else T.empty(shape, dtype=T.bool, device=dev) if done is None else T.empty_like(done))
+            whole = T.empty_like(scores, dtype=T.i32)
+            out = (T.empty_like(scores), whole, T.empty_like(whole), T.empty_like(scores, dtype=T.bool) if eos >= 0 else None)
             s.out_scores, s.out_parent, s.out_token = out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr()
         else:
             _refuse(len(out) == 4, "out must be (scores, parents, tokens, done)")
@@ -266,7 +267,8 @@ class KVCache:
             raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
         B, n = shape[0], shape[1]
         code, c = _type_of(T, k, "k"), self._view(T, table, B)
-        _type_of(T, v, "v")
+        if v.requires_grad:
+            _type_of(T, v, "v")
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -325,7 +327,7 @@ class KVCache:
             if need < 0:
                 _check(need)
             if out is None:
-                out = T.empty(shape, dtype=q.dtype, device=self.device)
+                out = T.empty_like(q) if q.is_contiguous() else T.empty(shape, dtype=q.dtype, device=self.device)
                 a.out = out.data_ptr()
             else:
                 a.out = _array(out, "out", q.dtype, shape, self.device)
