@@ -30,17 +30,13 @@ __device__ __forceinline__ double exp_d(double d) {  // d up to 700
 constexpr int kSelBuf = 64;    // candidates that a wave ranks at a time: one per lane
 constexpr int kSelLists = 64;  // lists that a wave joins: one per lane
 
-// A logit and its index as one number: the larger comes first (the larger logit, of equal ones the smaller index).
-typedef unsigned long long cand_t;
-constexpr cand_t kNoCand = (cand_t)0x007fffffu << 32;  // -inf at index 0x7fffffff; below it: nothing
-__device__ __forceinline__ cand_t make_cand(float v, int i) { return (cand_t)orderable(v) << 32 | (uint32_t)(0x7fffffff - i); }
-__device__ __forceinline__ float cand_value(cand_t c) { return from_orderable((uint32_t)(c >> 32)); }
-__device__ __forceinline__ int cand_index(cand_t c) { return 0x7fffffff - (int)(uint32_t)c; }
+// a logit and its index as one number (zeros of both signs are equal)
+__device__ __forceinline__ uint64_t make_cand(float v, int i) { return pack_cand(v + 0.f, i); }
 
-// What a wave knows of its part of a row: the `beam` best logits, in lanes 0 .. beam - 1 in order (kNoCand behind the last), and
+// What a wave knows of its part of a row: the `beam` best logits, in lanes 0 .. beam - 1 in order (no_cand() behind the last), and
 // sum exp(x - ref), each lane's share of it.
 struct RowPart {
-  cand_t best = kNoCand;
+  uint64_t best = no_cand();
   double sum = 0.;
   float ref = -INFINITY;
   bool bad = false;  // a NaN or +inf among them (of this lane)
@@ -67,27 +63,27 @@ __device__ __forceinline__ uint32_t nth_group(const GroupKeys &g, int nth) {
 }
 
 struct alignas(16) CandBuf {
-  cand_t c[kSelBuf];
+  uint64_t c[kSelBuf];
   GroupKeys group;
 };
 
-// The first n places of the buffer hold candidates: the best `beam` of them go to its first places in order, kNoCand behind the last.
-__device__ __forceinline__ cand_t rank_candidates(int n, int beam, CandBuf &buf) {
+// The first n places of the buffer hold candidates: the best `beam` of them go to its first places in order, no_cand() behind the last.
+__device__ __forceinline__ uint64_t rank_candidates(int n, int beam, CandBuf &buf) {
   const int lane = threadIdx.x & 63;
   wave_lds_order();
   if (lane >= n) buf.c[lane] = 0;
   wave_lds_order();
-  const cand_t own = buf.c[lane];
+  const uint64_t own = buf.c[lane];
   int rank = 0;
   for (int j = 0; j < n; j += 8)
 #pragma unroll
     for (int u = 0; u < 8; ++u) rank += buf.c[j + u] > own;
   wave_lds_order();
-  if (lane < beam) buf.c[lane] = kNoCand;  // (equal ones, places without a candidate, have one rank)
+  if (lane < beam) buf.c[lane] = no_cand();  // (equal ones, places without a candidate, have one rank)
   wave_lds_order();
   if (lane < n && rank < beam) buf.c[rank] = own;
   wave_lds_order();
-  const cand_t out = lane < beam ? buf.c[lane] : kNoCand;
+  const uint64_t out = lane < beam ? buf.c[lane] : no_cand();
   wave_lds_order();
   return out;
 }
@@ -119,7 +115,7 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
 #pragma unroll
   for (int e = 0; e < E; ++e) part.sum += exp_d((double)x[e] - ref);
 
-  const float last = readlane_f(cand_value(part.best), beam - 1);
+  const float last = readlane_f(cand_key(part.best), beam - 1);
   if (!(most > last)) return;  // equal ones come after those of the list, whose indices are smaller
   const float pair = fmaxf(top, dpp_f<kDppXor1>(top));
   wave_lds_order();
@@ -137,7 +133,7 @@ __device__ __forceinline__ void take_tile(const float (&x)[E], int base, int bea
       n += __popcll(at);
     }
   }
-  const int held = __popcll(__ballot(lane < beam && part.best > kNoCand));
+  const int held = __popcll(__ballot(lane < beam && part.best > no_cand()));
   if (n + held > kSelBuf) {
     uint32_t taken = 0;
     n = 0;
@@ -209,7 +205,7 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 
 // A list as it is handed on: the best of a part of a row and the sum of its exponentials.
 struct SelList {
-  cand_t c[kMaxBeam];
+  uint64_t c[kMaxBeam];
 };
 struct SelStat {
   double sum;  // NaN: a NaN or +inf among the logits
@@ -248,7 +244,7 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
   const int l = min(lane, n_lists - 1), k = l / parts;
   // everything that is read leaves at once (what a finished hypothesis' lists hold is not looked at)
   const SelStat st = stats[l];
-  cand_t c[kMaxBeam];
+  uint64_t c[kMaxBeam];
   __builtin_memcpy(c, lists[l].c, sizeof(c));
   const double score = a.scores[(int64_t)b * beam + k];
   const bool finished = a.done && a.done[(int64_t)b * beam + k];
@@ -266,11 +262,11 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     for (int p = 0; p < parts; ++p) sum += sh.sum[k * parts + p];
   }
   const double lse = (double)ref + log(sum);
-  if (finished) c[0] = lane == k * parts ? make_cand(0.f, a.eos) : kNoCand;  // its one candidate: eos, with the score that it has
+  if (finished) c[0] = lane == k * parts ? make_cand(0.f, a.eos) : no_cand();  // its one candidate: eos, with the score that it has
   // (a list's keys descend; NaN is none)
   const auto key_of = [&](int j) {
-    const double key = finished ? score : score + ((double)cand_value(c[j]) - lse);
-    return c[j] > kNoCand && key > -INFINITY && (j == 0 || !finished) && lane < n_lists ? key : -INFINITY;
+    const double key = finished ? score : score + ((double)cand_key(c[j]) - lse);
+    return c[j] > no_cand() && key > -INFINITY && (j == 0 || !finished) && lane < n_lists ? key : -INFINITY;
   };
   // the bound, in float32 rounded down
   const int firsts = max(min(64, 4 * beam) / n_lists, 1);
@@ -298,8 +294,8 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     if (in) {
       const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0));
       sh.key[pos] = key;
-      sh.token[pos] = cand_index(c[j]);
-      sh.x[pos] = cand_value(c[j]);
+      sh.token[pos] = cand_idx(c[j]);
+      sh.x[pos] = cand_key(c[j]);
       sh.k[pos] = (uint8_t)k;
     }
     n += __popcll(at);
@@ -392,7 +388,7 @@ __global__ __launch_bounds__(256, 5) void k_select_scan(SelectArgs a) {
   float ref = -INFINITY, last = -INFINITY;  // of the block's list: its beam-th
   bool bad = false, many = false;
   int held = 0;  // places of the list that are filled
-  if (threadIdx.x < kMaxBeam) sh.buf.c[threadIdx.x] = kNoCand;
+  if (threadIdx.x < kMaxBeam) sh.buf.c[threadIdx.x] = no_cand();
   const int ranker = blockIdx.x / 256 & 3;  // of the blocks that share a unit each another wave, so another SIMD
   for (int base = begin; base < end; base += 256 * E) {
     float x[E];
@@ -477,7 +473,7 @@ __global__ __launch_bounds__(256, 5) void k_select_scan(SelectArgs a) {
     if (base + 256 * E >= end) break;
     __syncthreads();
     if (n) held = beam;
-    last = cand_value(sh.buf.c[beam - 1]);
+    last = cand_key(sh.buf.c[beam - 1]);
   }
   sum = wave_sum_d(sum);
   if (lane == 0) sh.stat[wave].sum = __any(bad) ? (double)NAN : sum;

@@ -178,6 +178,21 @@ def test_scores_that_float32_does_not_hold(V):
     assert got[2][0].tolist() == logits[0, 0].topk(4).indices.tolist()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K,V", [(1, 50), (5, 900), (4, 9000), (16, 1500)])
+def test_zeros_of_both_signs_are_equal(K, V, dtype):
+    import torch
+    g = np.random.default_rng(V)
+    x = np.where(g.random((3, K, V)) < 0.5, -0.0, 0.0)
+    x[g.random(x.shape) < 0.4] = -1.0
+    x[1] = np.where(g.random((K, V)) < 0.01, x[1], -1.0)  # few of them
+    logits = torch.from_numpy(x).to(R.torch_type(dtype)).cuda()
+    scores = np.sort(g.random((3, K)))
+    want, got = R.select(x, scores), run(logits, scores)
+    np.testing.assert_array_equal(got[1], want[1])
+    np.testing.assert_array_equal(got[2], want[2])
+
+
 def test_the_longest_row():
     """Indices up to the last that is allowed; equal logits everywhere else."""
     import math
