@@ -401,8 +401,8 @@ typedef struct { /* rows of a network: [B, n, heads, dim], dim contiguous */
   int64_t stride_b, stride_n, stride_h;
 } rnnt_rows_t;
 
-/* Rows (b, i), i < count[b] (NULL: all n) to positions start[b] + i, and back.  Two rows written to one position: one of them.  Read rows
- * from count[b] on are zeros. */
+/* Rows (b, i), i < count[b] (NULL: all n) to positions start[b] + i, and back.  Equal rows may be written to one position (sequences that share a
+ * page), different ones leave no row in particular.  Read rows from count[b] on are zeros. */
 int rnnt_cache_write(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t *v, int32_t type, int32_t B, int32_t n,
                      const int32_t *start, const int32_t *count, void *hip_stream);
 int rnnt_cache_read(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_rows_t *v, int32_t type, int32_t B, int32_t n,

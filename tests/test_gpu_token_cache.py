@@ -140,6 +140,20 @@ def test_positions_and_pages_that_are_not_there():
     assert torch.equal(before, cache.k)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_equal_rows_written_to_one_position(fmt):
+    import torch
+    from paper_2506_00185_amd import KVCache
+    g = np.random.default_rng(31)
+    one, many = KVCache(3, 16, 2, 64, fmt), KVCache(3, 16, 2, 64, fmt)
+    k, v = (cuda(g.standard_normal((1, 40, 2, 64)), torch.bfloat16) for _ in range(2))
+    table, zero = cuda(np.array([[2, 0, 1]], np.int32)), cuda(np.zeros(50, np.int32))
+    one.write(k, v, table, zero[:1])
+    many.write(k.expand(50, -1, -1, -1), v.expand(50, -1, -1, -1), table.expand(50, -1), zero)
+    for a, b in zip((one.k, one.v, one.k_exp, one.v_exp), (many.k, many.v, many.k_exp, many.v_exp)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def test_strided_rows_and_another_stream():
     import torch
     from paper_2506_00185_amd import KVCache
