@@ -25,6 +25,7 @@ inline int launch(void (*kernel)(Args), int64_t blocks, int blocks_y, int thread
   void *params[] = {&copy};
   const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)blocks, (unsigned)blocks_y), dim3((unsigned)threads), params, 0, stream);
   if (e == hipSuccess) return RNNT_OK;
+  (void)hipGetLastError();  // (reported here, not again by the next call of other code)
   set_call_error(hipGetErrorString(e));
   return RNNT_E_HIP;
 }
