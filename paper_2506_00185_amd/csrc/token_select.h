@@ -268,8 +268,8 @@ __device__ __forceinline__ void join_lists(const SelectArgs &a, int b, const Sel
     const double key = finished ? score : score + ((double)cand_key(c[j]) - lse);
     return c[j] > no_cand() && key > -INFINITY && (j == 0 || !finished) && lane < n_lists ? key : -INFINITY;
   };
-  // the bound, in float32 rounded down
-  const int firsts = max(min(64, 4 * beam) / n_lists, 1);
+  // the bound, in float32 rounded down (a list has `beam` places, what lies behind them nobody wrote)
+  const int firsts = min(max(min(64, 4 * beam) / n_lists, 1), beam);
   sh.low[lane] = -INFINITY;
   wave_lds_order();
 #pragma unroll

@@ -75,6 +75,42 @@ def test_finished_hypotheses_and_empty_slots(K, V):
     assert np.isneginf(s).all() and (p == -1).all() and (t == -3).all() and not d.any()
 
 
+def run_in(fill, logits, scores, done=None, eos=-1):
+    """The C call with a workspace of the caller's that holds ``fill`` in every byte."""
+    import ctypes as C
+    import torch
+    from paper_2506_00185_amd import load_library
+    from paper_2506_00185_amd.tokens import _Select
+    lib, (B, K, V) = load_library(), logits.shape
+    assert logits.is_contiguous()
+    need = lib.rnnt_select_tokens_workspace(B, K, V)
+    assert need > 0
+    work = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+    s, d = torch.from_numpy(scores).cuda(), None if done is None else torch.from_numpy(done).cuda()
+    out = [torch.empty(B, K, dtype=t, device="cuda") for t in (torch.float64, torch.int32, torch.int32, torch.bool)]
+    code = [torch.float32, torch.float16, torch.bfloat16].index(logits.dtype)
+    a = _Select(C.sizeof(_Select), code, B, K, V, eos, logits.data_ptr(), K * V, V, s.data_ptr(), None if d is None else d.data_ptr(),
+                *(t.data_ptr() for t in out[:3]), out[3].data_ptr() if eos >= 0 else None, work.data_ptr(), need)
+    assert lib.rnnt_select_tokens(C.byref(a), C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+    return [t.cpu().numpy() for t in (out if eos >= 0 else out[:3])]
+
+
+# two launches with 1024 rows and more, so that lists are few: one to a row for beams from 3 on
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,K,V", [(342, 3, 5462), (400, 3, 8192), (1025, 1, 16400), (513, 2, 8200), (260, 4, 4200), (128, 9, 2000), (104, 10, 8192), (64, 16, 1100),
+                                   (64, 16, 8193)])
+def test_what_a_workspace_held_does_not_matter(B, K, V, dtype):
+    """Words that read as no candidate, as logits of 1.5 and 48.6, above most and all of the logits, and as NaN."""
+    logits, scores = make(B, K, V, dtype, B + K + V)
+    eos = V // 2
+    done = np.random.default_rng(V).random((B, K)) < 0.1
+    want = check(logits, scores, done, eos)
+    for fill in (0x00, 0xbf, 0xc2, 0xff):
+        for a, b in zip(run_in(fill, logits, scores, done, eos), want):
+            np.testing.assert_array_equal(a, b)
+
+
 def test_finished_hypotheses_logits_are_not_read():
     logits, scores = make(2, 4, 3000, "f32", 1)
     logits[:, 1] = float("nan")
