@@ -15,8 +15,8 @@ namespace rb {
 // Exponents: x = log2(e) scale q.k 2^(s_k) is the logit in base 2.  A value row's exponent is added to it: P' = 2^(x + s_v - M) is rounded to
 // float16 and multiplied by y_v as stored, and the soft-max's denominator sums P' 2^(-s_v).  P' is at most 2^15 and the largest of a row at
 // least 2^7: float16 keeps 11 bits of those down to 2^-21 of the largest.  Precision: Q is scaled by a power of two for each row and
-// rounded to float16 (bfloat16 values down to 2^-28 of the row's largest are exact), float32 Q as a sum of two float16; P' is one float16 where
-// the output is bfloat16, whose rounding is eight times as coarse, else a sum of two; sums are float32.
+// rounded to float16 (bfloat16 values down to 2^-28 of the row's largest are exact), float32 Q as a sum of two float16, and so is P', for all
+// types: with one, whose 11 bits are less than float32 keeps, outputs in bfloat16 were rounded to a neighbour now and then; sums are float32.
 // M follows the running maximum only when a logit passes it by 2^8 (the range that float16 leaves above), so that the accumulators are
 // multiplied by a correction a few times in a row of thousands of tokens.
 // Measured: one token for each of 32 sequences of 1000 to 8000, 32 heads on 8 of 128 in e4m3: 61 us and 4 for the join, 4.6 TB/s of a large copy's
@@ -121,7 +121,6 @@ struct Attend {
   typedef typename TT::T T;
   static constexpr int FB = FMT / 8;                       // bytes of a kept value
   static constexpr bool Q2 = std::is_same<T, float>::value;        // Q as two float16
-  static constexpr bool P2 = !std::is_same<T, uint16_t>::value;    // P' as two float16
   static constexpr int KS = DP / 32;                       // k-steps of Q.K
   static constexpr int KQ = DP / 4;                        // values of a key row that a lane holds
   static constexpr int VN = DP / 16;                       // values of a value row that a lane holds
@@ -442,7 +441,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
       for (int w = 0; w < 4; ++w) {
         const uint32_t hi = pack_f16(p[2 * w], p[2 * w + 1]);
         pb[m][w] = hi;
-        if constexpr (A::P2) pl[m][w] = pack_f16_rest(p[2 * w], p[2 * w + 1], hi);
+        pl[m][w] = pack_f16_rest(p[2 * w], p[2 * w + 1], hi);
       }
     }
     // four (two) dims at a time: the words of eight tokens that hold them, transposed
@@ -475,7 +474,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           acc[m][PER * w + i] = mfma16_f16(va[i], pb[m], acc[m][PER * w + i]);
-          if constexpr (A::P2) acc[m][PER * w + i] = mfma16_f16(va[i], pl[m], acc[m][PER * w + i]);
+          acc[m][PER * w + i] = mfma16_f16(va[i], pl[m], acc[m][PER * w + i]);
         }
     }
     next_values();

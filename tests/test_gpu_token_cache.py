@@ -284,6 +284,25 @@ def check(cache, table, q, lens, parents=None, scale=None, dtype="f32", **kw):
     return got
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim,heads,group,n", [(64, 2, 4, 1), (128, 2, 4, 1), (256, 1, 3, 1), (64, 2, 2, 9), (128, 2, 3, 40)])
+def test_bfloat16_outputs_are_rounded_once(fmt, dim, heads, group, n):
+    """No bits are lost ahead of the output's own rounding: it lies between the 64-bit result's rounded on either side of what `dim` products summed in float32,
+    the float32 exponent, p as two float16 (2^-22) and `tokens` float32 additions leave open (numerator and denominator, as in tolerance())."""
+    import torch
+    g = np.random.default_rng(dim + n)
+    lens = np.array([2, 5, 40, 300])
+    cache, table = filled(g, 4, 300 + n, heads, dim, fmt, 16)
+    q = cuda(g.standard_normal((4, n, heads * group, dim)), torch.bfloat16)
+    k, v = values_of(cache, table, 300 + n)
+    want, size, far = R.attend(q.double().cpu().numpy(), k, v, lens, [list(range(-1, n - 1))] * 4, dim**-0.5)
+    x = far[..., None] * dim * 2.0**-24 + (far[..., None] * 1.45 + 64) * 2.0**-23
+    open_ = size * (2 * (x + 2.0**-22) + 2.0**-22 + 2 * (300 + n) * 2.0**-24) + np.abs(want) * 2.0**-22  # (the last: want through float32 on its way)
+    low, high = (torch.from_numpy(want + s * open_).to(torch.bfloat16).double().numpy() for s in (-1, 1))
+    y = cache.attend(q, table, cuda(lens.astype(np.int32))).double().cpu().numpy()
+    assert (low <= y).all() and (y <= high).all(), int(((low > y) | (y > high)).sum())
+
+
 def some_tree(g, B, n, padded=True):
     i = np.arange(n)
     parents = np.maximum(i - 1 - (g.random((B, n)) ** 2 * 5).astype(int), -1)
