@@ -49,6 +49,12 @@ def _refuse(ok, what):
         raise RnntBeamError(what)
 
 
+def _sizes(*sizes):
+    """The library counts in 32 bits, and ctypes passes on the last 32 bits of what does not fit."""
+    if max(sizes) > 0x7fffffff:
+        raise RnntBeamError(f"sizes must be below 2^31, not {max(sizes)}")
+
+
 class _Torch:
     """What the calls below need of torch, looked up once: a call is a few microseconds in all."""
 
@@ -126,6 +132,9 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     stride_b, stride_k, stride_v = logits.stride()
     if V < 1 or (V > 1 and stride_v != 1):
         raise RnntBeamError("the last dimension of logits must be contiguous")
+    _sizes(B, beam, V)
+    if not -1 <= eos < V:
+        raise RnntBeamError("eos must be a token, or -1")
     dev, shape = logits.device, (B, beam)
     s = _Select(C.sizeof(_Select), _type_of(T, logits, "logits"), B, beam, V, eos, logits.data_ptr(), stride_b, stride_k,
                 _array(scores, "scores", T.f64, shape, dev))
@@ -192,6 +201,7 @@ def reorder_states(parents, states, lead=0, stream=None):
             raise RnntBeamError(f"state {i} must be [{'layers, ' * lead}B, beam, ...]")
         rows, stride, run = _rows_of(full[lead + 2:], strides[lead + 2:], i)
         outer, outer_stride = (full[0], strides[0]) if lead else (1, 0)
+        _sizes(outer, rows, *shape)
         views[i] = _States(t.data_ptr(), outer_stride * size, strides[lead] * size, strides[lead + 1] * size, stride * size, run * size, outer, rows)
     raw, scope = _enter(T, parents, stream, (parents, *states))
     try:
@@ -226,6 +236,7 @@ class KVCache:
     def _set(self, k, v, k_exp, v_exp):
         import torch
         _refuse(k.dim() == 4 and k.dtype in (torch.float16, torch.float8_e4m3fn), "k must be [n_pages, heads, page_size, dim], float8_e4m3fn or float16")
+        _sizes(*k.shape)
         _refuse(k.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
         self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
         self.n_pages, self.heads, self.page_size, self.dim = k.shape
@@ -243,6 +254,7 @@ class KVCache:
             _refuse(len(shape) == 2 and table.dtype == T.i32 and shape[0] == B and shape[1] >= 1, f"table must be int32 [{B}, width]")
             _refuse(table.device == self.device, f"table is on {table.device}, not on {self.device}")
             raise RnntBeamError("rows of table must be contiguous")
+        _sizes(B, shape[1])
         c = _Cache.from_buffer_copy(self._c)
         c.table, c.table_stride, c.width = table.data_ptr(), strides[0], shape[1]
         return c
@@ -253,6 +265,7 @@ class KVCache:
             _refuse(len(shape) == 4 and shape[2] == heads and shape[3] == self.dim, f"{what} must be [B, n, {heads}, {self.dim}]")
             _refuse(t.device == self.device, f"{what} is on {t.device}, not on {self.device}")
             raise RnntBeamError(f"the last dimension of {what} must be contiguous")
+        _sizes(shape[1], heads)
         return _Rows(t.data_ptr(), strides[0], strides[1], strides[2])
 
     def _counts(self, T, start, count, B):
@@ -285,6 +298,7 @@ class KVCache:
         dtype = dtype or T.f32
         code, B = T.types.get(dtype), table.shape[0]
         _refuse(code is not None, "dtype must be float32, float16 or bfloat16")
+        _sizes(n)
         c = self._view(T, table, B)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -314,10 +328,13 @@ class KVCache:
         c = self._view(T, table, B)
         rows = self._rows(q, "q", heads)
         bound = self.page_size * c.width if max_len is None else max_len
+        if bound < 0:
+            raise RnntBeamError("max_len must not be negative")
         a = _Attend(C.sizeof(_Attend), _type_of(T, q, "q"), B, n, n, heads, dim ** -0.5 if scale is None else scale, min(bound, 0x7fffffff), rows)
         a.lens = _array(lens, "lens", T.i32, (B,), self.device)
         if parents is not None:
             _refuse(parents.dim() == 2, "parents must be [B, tree]")
+            _sizes(parents.shape[1])
             a.tree = parents.shape[1]
             a.parents = _array(parents, "parents", T.i32, (B, a.tree), self.device)
         lib = T.lib
@@ -348,6 +365,7 @@ def nbest_tree(tokens, lens, max_nodes=None) -> dict:
     tokens, lens = np.ascontiguousarray(tokens, np.int32), np.ascontiguousarray(lens, np.int32)
     _refuse(tokens.ndim == 3 and lens.shape == tokens.shape[:2], "tokens must be [B, beam, cap], lens [B, beam]")
     B, beam, cap = tokens.shape
+    _sizes(B, beam, cap, max_nodes or 0)
     room = max(1, int(np.maximum(lens, 0).sum(1).max(initial=0))) if max_nodes is None else max_nodes
     tok, par = (np.empty((B, room), np.int32) for _ in range(2))
     leaf, n_nodes = np.empty((B, beam), np.int32), np.empty(B, np.int32)

@@ -199,6 +199,51 @@ def test_python_side_refuses_host_tensors():
         KVCache(1, 16, 1, 64, device="cpu")
 
 
+def a_meta_cache(n_pages=4, page_size=16, heads=2, dim=64):
+    """A cache whose tensors have shapes and no memory: calls get as far as the check of the device."""
+    import torch
+    from paper_2506_00185_amd import KVCache
+    from paper_2506_00185_amd.tokens import _Cache
+    c = KVCache.__new__(KVCache)
+    c.k = c.v = torch.empty(n_pages, heads, page_size, dim, dtype=torch.float16, device="meta")
+    c.k_exp = c.v_exp = torch.empty(n_pages, heads, page_size, dtype=torch.uint8, device="meta")
+    c.n_pages, c.heads, c.page_size, c.dim, c.device, c.format = n_pages, heads, page_size, dim, c.k.device, "f16"
+    c._c = _Cache(struct_size=C.sizeof(_Cache), format=1, n_pages=n_pages, page_size=page_size, heads=heads, dim=dim)
+    return c
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused(lib):
+    """(The library counts in 32 bits: passed on, 2^32 + 5 would be 5.)"""
+    import torch
+    from paper_2506_00185_amd import KVCache, RnntBeamError, nbest_tree, reorder_states, select_tokens
+    big = 2**32 + 5
+    meta = lambda *shape, dtype=torch.float16: torch.empty(shape, dtype=dtype, device="meta")  # noqa: E731
+    i32, f64 = torch.int32, torch.float64
+    c = a_meta_cache()
+    table, start, rows = meta(3, 8, dtype=i32), meta(3, dtype=i32), meta(3, 5, 2, 64)
+    states = [(meta(2, 3, big), 0), (meta(2, 3, big, 2)[..., :1], 0), (meta(big, 2, 3, 4), 1)]
+    calls = [lambda: select_tokens(meta(2, 3, big), meta(2, 3, dtype=f64)), lambda: select_tokens(meta(big, 3, 7), meta(big, 3, dtype=f64)),
+             lambda: KVCache.from_tensors(meta(big, 1, 1, 16), meta(big, 1, 1, 16), meta(big, 1, 1), meta(big, 1, 1)),
+             lambda: c.write(meta(3, big, 2, 64), meta(3, big, 2, 64), table, start), lambda: c.read(table, start, big),
+             lambda: c.write(rows, rows, meta(3, big, dtype=i32), start), lambda: c.write(meta(big, 1, 2, 64), meta(big, 1, 2, 64), meta(big, 8, dtype=i32), meta(big, dtype=i32)),
+             lambda: c.attend(meta(3, big, 2, 64), table, start), lambda: c.attend(meta(3, 1, big - 1, 64), table, start),
+             lambda: c.attend(rows, table, start, parents=meta(3, big, dtype=i32)),
+             lambda: nbest_tree(np.zeros((1, 1, 4), np.int32), np.ones((1, 1), np.int32), max_nodes=big),
+             lambda: nbest_tree(np.broadcast_to(np.int32(0), (1, 0, big)), np.zeros((1, 0), np.int32))]
+    calls += [lambda t=t, lead=lead: reorder_states(meta(2, 3, dtype=i32), [t], lead=lead) for t, lead in states[1:]]
+    for i, call in enumerate(calls):
+        with pytest.raises(RnntBeamError, match="2\\^31"):
+            call()
+            raise AssertionError(i)
+    with pytest.raises(RnntBeamError, match="GPU"):  # one run of so many elements is counted in 64 bits
+        reorder_states(meta(2, 3, dtype=i32), [states[0][0]])
+    for eos in (2**32 + 3, 3 - 2**32, 7, -2):
+        with pytest.raises(RnntBeamError, match="eos"):
+            select_tokens(meta(2, 3, 7), meta(2, 3, dtype=f64), eos=eos)
+    with pytest.raises(RnntBeamError, match="max_len"):
+        c.attend(rows, table, start, max_len=3 - 2**32)
+
+
 # ---------------------------------------------------------------- the plain implementations themselves
 def test_plain_formats():
     import torch
