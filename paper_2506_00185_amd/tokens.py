@@ -358,15 +358,26 @@ class KVCache:
         return out
 
 
+def _int32(a, what):
+    """A contiguous int32 array of the same numbers."""
+    a = np.asarray(a)
+    with np.errstate(invalid="ignore"):
+        out = np.ascontiguousarray(a, np.int32)
+    _refuse(a.dtype == np.int32 or bool((out == a).all()), f"{what} must be int32, or numbers that it holds")
+    return out
+
+
 def nbest_tree(tokens, lens, max_nodes=None) -> dict:
     """rnnt_nbest_tree: the prefix trees of the n-best lists of BeamDecoder.results (tokens [B, beam, cap], lens [B, beam], numpy), to be
     rescored by one KVCache.attend: tokens and parents [B, nodes] (parent -1: first token, -2: padding), leaf [B, beam]: the node at which each
     hypothesis ends (-1: empty), n_nodes [B]."""
-    tokens, lens = np.ascontiguousarray(tokens, np.int32), np.ascontiguousarray(lens, np.int32)
+    tokens, lens = _int32(tokens, "tokens"), _int32(lens, "lens")
     _refuse(tokens.ndim == 3 and lens.shape == tokens.shape[:2], "tokens must be [B, beam, cap], lens [B, beam]")
     B, beam, cap = tokens.shape
-    _sizes(B, beam, cap, max_nodes or 0)
-    room = max(1, int(np.maximum(lens, 0).sum(1).max(initial=0))) if max_nodes is None else max_nodes
+    _sizes(B, beam, cap)
+    # (lengths beyond cap are refused below)
+    room = max(1, int(np.clip(lens, 0, cap).sum(1, dtype=np.int64).max(initial=0))) if max_nodes is None else max_nodes
+    _sizes(room)
     tok, par = (np.empty((B, room), np.int32) for _ in range(2))
     leaf, n_nodes = np.empty((B, beam), np.int32), np.empty(B, np.int32)
     most = _check(load_library().rnnt_nbest_tree(*(C.c_void_p(x.ctypes.data) for x in (tokens, lens)), B, beam, cap, room,

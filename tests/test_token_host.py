@@ -244,6 +244,20 @@ def test_sizes_that_32_bits_do_not_hold_are_refused(lib):
         c.attend(rows, table, start, max_len=3 - 2**32)
 
 
+def test_prefix_trees_of_other_integers():
+    from paper_2506_00185_amd import RnntBeamError, nbest_tree
+    tokens, lens = np.array([[[1, 2], [1, 3]]]), np.array([[2, 2]])
+    want = nbest_tree(tokens.astype(np.int32), lens.astype(np.int32))
+    for dtype in (np.int64, np.uint8, np.int16, np.float32):
+        got = nbest_tree(tokens.astype(dtype), lens.astype(dtype))
+        assert all(np.array_equal(got[k], want[k]) for k in want)
+    for t, n in [(tokens + 2**32, lens), (tokens, lens + 2**32), (tokens + 0.5, lens), (tokens, lens * 0.75), (tokens * np.nan, lens)]:
+        with pytest.raises(RnntBeamError, match="int32"):
+            nbest_tree(t, n)
+    with pytest.raises(RnntBeamError, match="beyond cap"):  # (and no room is made for such a length)
+        nbest_tree(tokens, lens + 2**30)
+
+
 # ---------------------------------------------------------------- the plain implementations themselves
 def test_plain_formats():
     import torch
