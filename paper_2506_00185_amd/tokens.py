@@ -3,7 +3,7 @@ rnnt_cache_write / read / attend and rnnt_nbest_tree.  Argument checks and marsh
 
 Tensors live on one GPU; work goes to ``stream`` (default: the current stream of that GPU) and the calls return without
 waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph.  The calls are for
-inference: a tensor that requires a gradient is refused."""
+inference: a tensor that requires a gradient is refused, among the outputs and what is overwritten too, unless gradients are off."""
 from __future__ import annotations
 
 import contextlib
@@ -85,9 +85,13 @@ def _type_of(T, t, what):
     code = T.types.get(t.dtype)
     if code is None:
         raise RnntBeamError(f"{what} must be float32, float16 or bfloat16")
-    if t.requires_grad and T.grads():
-        raise RnntBeamError(f"{what} requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
     return code
+
+
+def _no_gradients(T, *tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad and T.grads():
+            raise RnntBeamError("a tensor requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
 
 
 def _array(t, what, dtype, shape, device):
@@ -135,6 +139,7 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     _sizes(B, beam, V)
     if not -1 <= eos < V:
         raise RnntBeamError("eos must be a token, or -1")
+    _no_gradients(T, logits, scores, *(out or ()))
     dev, shape = logits.device, (B, beam)
     s = _Select(C.sizeof(_Select), _type_of(T, logits, "logits"), B, beam, V, eos, logits.data_ptr(), stride_b, stride_k,
                 _array(scores, "scores", T.f64, shape, dev))
@@ -193,6 +198,7 @@ def reorder_states(parents, states, lead=0, stream=None):
     ptr = _array(parents, "parents", T.i32, shape, dev)
     _refuse(lead in (0, 1), "lead must be 0 or 1")
     _refuse(len(states) <= 16, "at most 16 tensors")
+    _no_gradients(T, *states)
     views = (_States * max(len(states), 1))()
     for i, t in enumerate(states):
         full, strides, size = t.shape, t.stride(), t.element_size()
@@ -280,8 +286,7 @@ class KVCache:
             raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
         B, n = shape[0], shape[1]
         code, c = _type_of(T, k, "k"), self._view(T, table, B)
-        if v.requires_grad:
-            _type_of(T, v, "v")
+        _no_gradients(T, k, v, self.k, self.v)
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -299,6 +304,7 @@ class KVCache:
         code, B = T.types.get(dtype), table.shape[0]
         _refuse(code is not None, "dtype must be float32, float16 or bfloat16")
         _sizes(n)
+        _no_gradients(T, self.k, self.v)
         c = self._view(T, table, B)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -325,6 +331,7 @@ class KVCache:
         if len(shape) != 4:
             raise RnntBeamError("q must be [B, n, q_heads, dim]")
         B, n, heads, dim = shape
+        _no_gradients(T, q, self.k, self.v, out)
         c = self._view(T, table, B)
         rows = self._rows(q, "q", heads)
         bound = self.page_size * c.width if max_len is None else max_len

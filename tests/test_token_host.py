@@ -244,6 +244,51 @@ def test_sizes_that_32_bits_do_not_hold_are_refused(lib):
         c.attend(rows, table, start, max_len=3 - 2**32)
 
 
+def differentiable_calls():
+    """(call, floating tensors by name) for each call; ``call`` takes what replaces one of them."""
+    import torch
+    from paper_2506_00185_amd import reorder_states, select_tokens
+    meta = lambda *shape, dtype=torch.float16: torch.empty(shape, dtype=dtype, device="meta")  # noqa: E731
+    i32, f64 = torch.int32, torch.float64
+    table, start, parents = meta(3, 8, dtype=i32), meta(3, dtype=i32), meta(2, 3, dtype=i32)
+
+    def cache_call(name):
+        def call(kk=None, vv=None, a=None, b=None, out=None):
+            c = a_meta_cache()
+            c.k, c.v = c.k if kk is None else kk, c.v if vv is None else vv
+            rows = [meta(3, 5, 2, 64) if t is None else t for t in (a, b)]
+            if name == "write":
+                c.write(*rows, table, start)
+            elif name == "read":
+                c.read(table, start, 5)
+            else:
+                c.attend(rows[0], table, start, out=out)
+        return call
+
+    cache, rows = dict(kk=meta(4, 2, 16, 64), vv=meta(4, 2, 16, 64)), meta(3, 5, 2, 64)
+    return {"select": (lambda x=meta(2, 3, 7), s=meta(2, 3, dtype=f64), o=meta(2, 3, dtype=f64): select_tokens(x, s, out=(o, parents, parents, None)),
+                       dict(x=meta(2, 3, 7), s=meta(2, 3, dtype=f64), o=meta(2, 3, dtype=f64))),
+            "reorder": (lambda x=meta(2, 3, 4): reorder_states(parents, [meta(2, 3), x]), dict(x=meta(2, 3, 4))),
+            "write": (cache_call("write"), dict(cache, a=rows, b=rows)), "read": (cache_call("read"), cache),
+            "attend": (cache_call("attend"), dict(cache, a=rows, out=rows))}
+
+
+@pytest.mark.parametrize("name", ["select", "reorder", "write", "read", "attend"])
+def test_tensors_that_require_a_gradient_are_refused(name):
+    import torch
+    from paper_2506_00185_amd import RnntBeamError
+    call, tensors = differentiable_calls()[name]
+    for k, t in tensors.items():
+        leaf = torch.empty_like(t, requires_grad=True)
+        for x in (leaf, leaf * 1.0, leaf.view_as(leaf)):
+            with pytest.raises(RnntBeamError, match="gradient"):
+                call(**{k: x})
+            with torch.no_grad(), pytest.raises(RnntBeamError, match="GPU"):
+                call(**{k: x})
+            with pytest.raises(RnntBeamError, match="GPU"):
+                call(**{k: x.detach()})
+
+
 def test_prefix_trees_of_other_integers():
     from paper_2506_00185_amd import RnntBeamError, nbest_tree
     tokens, lens = np.array([[[1, 2], [1, 3]]]), np.array([[2, 2]])
