@@ -3,7 +3,8 @@ rnnt_cache_write / read / attend and rnnt_nbest_tree.  Argument checks and marsh
 
 Tensors live on one GPU; work goes to ``stream`` (default: the current stream of that GPU) and the calls return without
 waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph.  The calls are for
-inference: a tensor that requires a gradient is refused, among the outputs and what is overwritten too, unless gradients are off."""
+inference: a tensor that requires a gradient is refused, among the outputs and what is overwritten too, unless gradients are off; one with a tangent of
+forward differentiation always."""
 from __future__ import annotations
 
 import contextlib
@@ -60,11 +61,12 @@ class _Torch:
 
     def __init__(self):
         import torch
+        import torch.autograd.forward_ad as forward
         # (of equals the faster one: a tensor like another, the device's number without a check that there is a device)
         self.empty, self.empty_like = torch.empty, torch.empty_like
         self.device_of = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.f64, self.f32, self.i32, self.u8, self.bool = torch.float64, torch.float32, torch.int32, torch.uint8, torch.bool
-        self.grads = torch.is_grad_enabled
+        self.grads, self.forward = torch.is_grad_enabled, forward
         self.types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         # (the pointer alone where this torch gives it without an object around it)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -88,10 +90,14 @@ def _type_of(T, t, what):
     return code
 
 
-def _no_gradients(T, *tensors):
+def _no_derivatives(T, *tensors):
     for t in tensors:
         if t is not None and t.requires_grad and T.grads():
             raise RnntBeamError("a tensor requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
+    if T.forward._current_level >= 0:
+        for t in tensors:
+            if t is not None and T.forward.unpack_dual(t).tangent is not None:
+                raise RnntBeamError("a tensor has a tangent, of which this call has none: take its primal")
 
 
 def _array(t, what, dtype, shape, device):
@@ -139,7 +145,7 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     _sizes(B, beam, V)
     if not -1 <= eos < V:
         raise RnntBeamError("eos must be a token, or -1")
-    _no_gradients(T, logits, scores, *(out or ()))
+    _no_derivatives(T, logits, scores, *(out or ()))
     dev, shape = logits.device, (B, beam)
     s = _Select(C.sizeof(_Select), _type_of(T, logits, "logits"), B, beam, V, eos, logits.data_ptr(), stride_b, stride_k,
                 _array(scores, "scores", T.f64, shape, dev))
@@ -198,7 +204,7 @@ def reorder_states(parents, states, lead=0, stream=None):
     ptr = _array(parents, "parents", T.i32, shape, dev)
     _refuse(lead in (0, 1), "lead must be 0 or 1")
     _refuse(len(states) <= 16, "at most 16 tensors")
-    _no_gradients(T, *states)
+    _no_derivatives(T, *states)
     views = (_States * max(len(states), 1))()
     for i, t in enumerate(states):
         full, strides, size = t.shape, t.stride(), t.element_size()
@@ -286,7 +292,7 @@ class KVCache:
             raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
         B, n = shape[0], shape[1]
         code, c = _type_of(T, k, "k"), self._view(T, table, B)
-        _no_gradients(T, k, v, self.k, self.v)
+        _no_derivatives(T, k, v, self.k, self.v)
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -304,7 +310,7 @@ class KVCache:
         code, B = T.types.get(dtype), table.shape[0]
         _refuse(code is not None, "dtype must be float32, float16 or bfloat16")
         _sizes(n)
-        _no_gradients(T, self.k, self.v)
+        _no_derivatives(T, self.k, self.v)
         c = self._view(T, table, B)
         first, many = self._counts(T, start, count, B)
         raw, scope = _enter(T, self.k, stream, (table, start, count, self.k, self.v, self.k_exp, self.v_exp))
@@ -331,7 +337,7 @@ class KVCache:
         if len(shape) != 4:
             raise RnntBeamError("q must be [B, n, q_heads, dim]")
         B, n, heads, dim = shape
-        _no_gradients(T, q, self.k, self.v, out)
+        _no_derivatives(T, q, self.k, self.v, out)
         c = self._view(T, table, B)
         rows = self._rows(q, "q", heads)
         bound = self.page_size * c.width if max_len is None else max_len

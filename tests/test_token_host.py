@@ -289,6 +289,22 @@ def test_tensors_that_require_a_gradient_are_refused(name):
                 call(**{k: x.detach()})
 
 
+@pytest.mark.parametrize("name", ["select", "reorder", "write", "read", "attend"])
+def test_forward_tangents_are_refused(name):
+    import torch
+    import torch.autograd.forward_ad as fw
+    from paper_2506_00185_amd import RnntBeamError
+    call, tensors = differentiable_calls()[name]
+    for k, t in tensors.items():
+        with fw.dual_level():
+            dual = fw.make_dual(t, torch.empty_like(t))
+            for guard in (torch.enable_grad, torch.no_grad):
+                with guard(), pytest.raises(RnntBeamError, match="tangent"):
+                    call(**{k: dual})
+            with pytest.raises(RnntBeamError, match="GPU"):
+                call(**{k: t})
+
+
 def test_prefix_trees_of_other_integers():
     from paper_2506_00185_amd import RnntBeamError, nbest_tree
     tokens, lens = np.array([[[1, 2], [1, 3]]]), np.array([[2, 2]])
