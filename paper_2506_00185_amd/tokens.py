@@ -4,7 +4,7 @@ rnnt_cache_write / read / attend and rnnt_nbest_tree.  Argument checks and marsh
 Tensors live on one GPU; work goes to ``stream`` (default: the current stream of that GPU) and the calls return without
 waiting.  Outputs and workspaces are torch tensors of that stream, so that all calls may be captured into a graph.  The calls are for
 inference: a tensor that requires a gradient is refused, among the outputs and what is overwritten too, unless gradients are off; one with a tangent of
-forward differentiation always."""
+forward differentiation always.  What a call overwrites counts as changed in place: a backward pass that saved it says so."""
 from __future__ import annotations
 
 import contextlib
@@ -50,10 +50,13 @@ def _refuse(ok, what):
         raise RnntBeamError(what)
 
 
-def _sizes(*sizes):
+_MOST = 0x7fffffff
+
+
+def _sizes(a, b=0, c=0):
     """The library counts in 32 bits, and ctypes passes on the last 32 bits of what does not fit."""
-    if max(sizes) > 0x7fffffff:
-        raise RnntBeamError(f"sizes must be below 2^31, not {max(sizes)}")
+    if a > _MOST or b > _MOST or c > _MOST:
+        raise RnntBeamError(f"sizes must be below 2^31, not {max(a, b, c)}")
 
 
 class _Torch:
@@ -68,6 +71,7 @@ class _Torch:
         self.f64, self.f32, self.i32, self.u8, self.bool = torch.float64, torch.float32, torch.int32, torch.uint8, torch.bool
         self.grads, self.forward = torch.is_grad_enabled, forward
         self.types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        self.changed = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
         # (the pointer alone where this torch gives it without an object around it)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.lib = load_library()
@@ -91,9 +95,10 @@ def _type_of(T, t, what):
 
 
 def _no_derivatives(T, *tensors):
-    for t in tensors:
-        if t is not None and t.requires_grad and T.grads():
-            raise RnntBeamError("a tensor requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
+    if T.grads():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise RnntBeamError("a tensor requires a gradient, of which this call has none: detach it, or call under torch.no_grad()")
     if T.forward._current_level >= 0:
         for t in tensors:
             if t is not None and T.forward.unpack_dual(t).tangent is not None:
@@ -152,6 +157,7 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
     if done is not None:
         s.done = _array(done, "done", T.bool, shape, dev)
     raw, scope = _enter(T, logits, stream, (logits, scores, done) + tuple(out or ()))
+    given = out
     try:
         if out is None:
             whole = T.empty_like(scores, dtype=T.i32)
@@ -171,6 +177,8 @@ def select_tokens(logits, scores, done=None, eos=-1, out=None, stream=None):
             work = T.empty(need, dtype=T.u8, device=dev)
             s.workspace, s.workspace_bytes = work.data_ptr(), need
         _check(T.lib.rnnt_select_tokens(C.byref(s), raw))
+        if given is not None:
+            T.changed([t for t in out if t is not None])
     finally:
         if scope:
             scope.close()
@@ -205,6 +213,7 @@ def reorder_states(parents, states, lead=0, stream=None):
     _refuse(lead in (0, 1), "lead must be 0 or 1")
     _refuse(len(states) <= 16, "at most 16 tensors")
     _no_derivatives(T, *states)
+    _sizes(shape[0])
     views = (_States * max(len(states), 1))()
     for i, t in enumerate(states):
         full, strides, size = t.shape, t.stride(), t.element_size()
@@ -213,11 +222,12 @@ def reorder_states(parents, states, lead=0, stream=None):
             raise RnntBeamError(f"state {i} must be [{'layers, ' * lead}B, beam, ...]")
         rows, stride, run = _rows_of(full[lead + 2:], strides[lead + 2:], i)
         outer, outer_stride = (full[0], strides[0]) if lead else (1, 0)
-        _sizes(outer, rows, *shape)
+        _sizes(outer, rows)
         views[i] = _States(t.data_ptr(), outer_stride * size, strides[lead] * size, strides[lead + 1] * size, stride * size, run * size, outer, rows)
     raw, scope = _enter(T, parents, stream, (parents, *states))
     try:
         _check(T.lib.rnnt_reorder_states(C.c_void_p(ptr), shape[0], shape[1], views, len(states), raw))
+        T.changed(states)
     finally:
         if scope:
             scope.close()
@@ -248,10 +258,11 @@ class KVCache:
     def _set(self, k, v, k_exp, v_exp):
         import torch
         _refuse(k.dim() == 4 and k.dtype in (torch.float16, torch.float8_e4m3fn), "k must be [n_pages, heads, page_size, dim], float8_e4m3fn or float16")
-        _sizes(*k.shape)
+        _sizes(k.shape[0], k.shape[1])
         _refuse(k.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
         self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
         self.n_pages, self.heads, self.page_size, self.dim = k.shape
+        self._written = (k, v, k_exp, v_exp)
         self.format = "f16" if k.dtype == torch.float16 else "e4m3"
         self._c = _Cache(struct_size=C.sizeof(_Cache), format=_FORMATS[self.format], n_pages=self.n_pages, page_size=self.page_size,
                          heads=self.heads, dim=self.dim)
@@ -277,7 +288,6 @@ class KVCache:
             _refuse(len(shape) == 4 and shape[2] == heads and shape[3] == self.dim, f"{what} must be [B, n, {heads}, {self.dim}]")
             _refuse(t.device == self.device, f"{what} is on {t.device}, not on {self.device}")
             raise RnntBeamError(f"the last dimension of {what} must be contiguous")
-        _sizes(shape[1], heads)
         return _Rows(t.data_ptr(), strides[0], strides[1], strides[2])
 
     def _counts(self, T, start, count, B):
@@ -291,6 +301,7 @@ class KVCache:
         if k.dtype != v.dtype or shape != v.shape or len(shape) != 4:
             raise RnntBeamError(f"k and v must be [B, n, {self.heads}, {self.dim}] of one type and shape")
         B, n = shape[0], shape[1]
+        _sizes(n)
         code, c = _type_of(T, k, "k"), self._view(T, table, B)
         _no_derivatives(T, k, v, self.k, self.v)
         rk, rv = self._rows(k, "k", self.heads), self._rows(v, "v", self.heads)
@@ -298,6 +309,7 @@ class KVCache:
         raw, scope = _enter(T, k, stream, (k, v, table, start, count, self.k, self.v, self.k_exp, self.v_exp))
         try:
             _check(T.lib.rnnt_cache_write(C.byref(c), C.byref(rk), C.byref(rv), code, B, n, first, many, raw))
+            T.changed(self._written)
         finally:
             if scope:
                 scope.close()
@@ -337,13 +349,14 @@ class KVCache:
         if len(shape) != 4:
             raise RnntBeamError("q must be [B, n, q_heads, dim]")
         B, n, heads, dim = shape
+        _sizes(n, heads)
         _no_derivatives(T, q, self.k, self.v, out)
         c = self._view(T, table, B)
         rows = self._rows(q, "q", heads)
         bound = self.page_size * c.width if max_len is None else max_len
         if bound < 0:
             raise RnntBeamError("max_len must not be negative")
-        a = _Attend(C.sizeof(_Attend), _type_of(T, q, "q"), B, n, n, heads, dim ** -0.5 if scale is None else scale, min(bound, 0x7fffffff), rows)
+        a = _Attend(C.sizeof(_Attend), _type_of(T, q, "q"), B, n, n, heads, dim ** -0.5 if scale is None else scale, min(bound, _MOST), rows)
         a.lens = _array(lens, "lens", T.i32, (B,), self.device)
         if parents is not None:
             _refuse(parents.dim() == 2, "parents must be [B, tree]")
@@ -353,6 +366,7 @@ class KVCache:
         lib = T.lib
         raw, scope = _enter(T, q, stream, (q, table, lens, parents, out, self.k, self.v, self.k_exp, self.v_exp))
         try:
+            given = out
             need = lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(a))
             if need < 0:
                 _check(need)
@@ -365,6 +379,8 @@ class KVCache:
                 work = T.empty(need, dtype=T.u8, device=self.device)
                 a.workspace, a.workspace_bytes = work.data_ptr(), need
             _check(lib.rnnt_cache_attend(C.byref(c), C.byref(a), raw))
+            if given is not None:
+                T.changed((out,))
         finally:
             if scope:
                 scope.close()

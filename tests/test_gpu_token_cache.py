@@ -236,6 +236,42 @@ def test_what_the_cache_refuses():
         KVCache.from_tensors(c.k, c.v, c.k_exp.int(), c.v_exp)
 
 
+def test_what_is_overwritten_counts_as_changed():
+    """Tensors that a backward pass has saved: it says that they were changed in place."""
+    import torch
+    from paper_2506_00185_amd import KVCache, reorder_states, select_tokens
+    g = np.random.default_rng(5)
+    table, start = cuda(np.array([[0, 1], [2, 3]], np.int32)), cuda(np.zeros(2, np.int32))
+    cache = KVCache(4, 16, 2, 64, "f16")
+    own = KVCache.from_tensors(cache.k[:], cache.v, cache.k_exp, cache.v_exp)  # (a view counts with what it is a view of)
+    k = cuda(g.standard_normal((2, 5, 2, 64)), torch.float32)
+    s, d = torch.zeros(2, 3, dtype=torch.float64, device="cuda"), torch.zeros(2, 3, dtype=torch.bool, device="cuda")
+    p, t = (torch.zeros(2, 3, dtype=torch.int32, device="cuda") for _ in range(2))
+    x, out, state = torch.randn(2, 3, 9, device="cuda"), torch.zeros(2, 5, 4, 64, device="cuda"), torch.randn(2, 3, 7, device="cuda")
+    q = torch.randn(2, 5, 4, 64, device="cuda")
+    calls = [(lambda: own.write(k, k, table, start), [cache.k, cache.v, cache.k_exp, cache.v_exp]), (lambda: cache.attend(q, table, start, out=out), [out]),
+             (lambda: select_tokens(x, s, d, 3, out=(s, p, t, d)), [s, p, t, d]), (lambda: reorder_states(torch.zeros_like(p), [state]), [state])]
+    for call, changed in calls:
+        call()
+        graphs = [(torch.ones(1, device="cuda", requires_grad=True) * y).sum() for y in changed]
+        before = [y._version for y in changed]
+        with torch.no_grad():
+            call()
+        assert all(y._version > n for y, n in zip(changed, before))
+        for graph in graphs:
+            with pytest.raises(RuntimeError, match="inplace"):
+                graph.backward()
+    before = [y._version for y in (cache.k, cache.v, q, x, k)]
+    cache.read(table, start, 5)
+    cache.attend(q, table, start)
+    select_tokens(x, torch.zeros_like(s))
+    assert before == [y._version for y in (cache.k, cache.v, q, x, k)]
+    with torch.inference_mode():
+        mine = torch.zeros(2, 3, 4, device="cuda")
+        reorder_states(p, [mine, state])
+    torch.cuda.synchronize()
+
+
 # ---------------------------------------------------------------- attention
 def filled(g, B, tokens, heads, dim, fmt, page, uneven=1.0):
     import torch
