@@ -366,7 +366,7 @@ int rnnt_select_tokens(const rnnt_select_t *args, void *hip_stream);
 /*
  * The states of hypotheses moved to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]] for every tensor, as if all
  * were read before any is written.  Parents outside 0 .. beam - 1 (an empty slot's -1) leave the slot as it is.  Up to 16 tensors
- * [lead, B, beam, inner, row_bytes]; rows that overlap are refused, tensors of one call must not overlap each other.
+ * [lead, B, beam, inner, row_bytes]; rows that overlap are refused, parent in one of them too; tensors of one call must not overlap each other.
  */
 typedef struct {
   void *data;

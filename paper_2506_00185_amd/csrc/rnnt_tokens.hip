@@ -1,4 +1,5 @@
 // Host side of the selection from a caller's logits and of the reordering of states.  See include/rnnt_beam.h for the contract.
+#include <algorithm>
 #include <new>
 #include <unordered_map>
 
@@ -53,6 +54,23 @@ int select_typed(const SelectArgs &a, bool one, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.B * a.beam * a.parts;
   const int rc = launch(a.part_len <= 2048 ? k_select_scan<TT, 8> : a.part_len <= 4096 ? k_select_scan<TT, 16> : k_select_scan<TT, 32>, blocks, 1, 256, a, stream);
   return rc ? rc : launch(k_select_join, a.B, 1, 64, a, stream);
+}
+
+// Whether a row of the tensor reaches into the `bytes` from `first` on.  (Rows do not overlap: of those that begin before their end, the last would.)
+bool holds(const rnnt_states_t &s, int B, int beam, const void *first, int64_t bytes) {
+  int64_t size[4] = {s.lead, B, beam, s.inner}, stride[4] = {s.lead_stride, s.b_stride, s.slot_stride, s.inner_stride};
+  int64_t behind = (int64_t)((uintptr_t)first - (uintptr_t)s.data) + bytes - 1;  // how far the last byte lies behind a row's beginning
+  if (behind < 0) return false;
+  bool done[4] = {};
+  for (int i = 0; i < 4; ++i) {
+    int top = -1;
+    for (int j = 0; j < 4; ++j)
+      if (!done[j] && size[j] > 1 && (top < 0 || stride[j] > stride[top])) top = j;
+    if (top < 0) break;
+    done[top] = true;
+    behind -= stride[top] * std::min(behind / stride[top], size[top] - 1);
+  }
+  return behind - (bytes - 1) < s.row_bytes;
 }
 
 int64_t select_lists(int B, int beam, const SelectPlan &p) { return p.one ? 0 : (int64_t)B * beam * p.parts; }
@@ -161,10 +179,12 @@ int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rn
     }
     v.chunks = (int)chunks;
     v.first_block = (int)blocks;
-    blocks += count;
-    if (blocks > 0x7fffffff) return refuse("more work than one launch takes");
+    blocks += count;  // (up to 16 such: the launch refuses what is too much)
   }
   if (!a.n || beam == 1) return RNNT_OK;
+  for (int t = 0; t < n; ++t)  // all blocks read the parents
+    if (states[t].lead && states[t].inner && states[t].row_bytes && holds(states[t], B, beam, parent, (int64_t)B * beam * (int64_t)sizeof(int32_t)))
+      return refuse("parents lie in a tensor that is reordered");
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (beam <= 4) return launch(k_reorder<4>, blocks, 1, 256, a, stream);
   if (beam <= 8) return launch(k_reorder<8>, blocks, 1, 256, a, stream);

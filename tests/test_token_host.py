@@ -123,6 +123,36 @@ def test_reordering_refuses_counts_and_repeats(lib):
     assert lib.rnnt_reorder_states(C.c_void_p(FAKE), 2, 4, empty, 1, None) == 0
 
 
+def test_reordering_refuses_parents_that_it_would_move(lib):
+    """(Other tensors' blocks would read parents while they are rewritten.)  A second tensor is more work than one launch takes, so that what is not refused for
+    its parents is refused for that, behind it."""
+    far = a_state(data=1 << 45, row_bytes=16, lead=2**30 - 1, lead_stride=16, slot_stride=1 << 34, b_stride=1 << 36)
+
+    def refused(at, **over):
+        assert lib.rnnt_reorder_states(C.c_void_p(at), 2, 4, (type(far) * 2)(a_state(**over), far), 2, None) == E_ARG
+        assert message(lib) in ("parents lie in a tensor that is reordered", "more work than one launch takes")
+        return "parents" in message(lib)
+
+    for at in (FAKE, FAKE + 400, FAKE + 7999, FAKE - 31):  # 2 x 4 rows of 1000 bytes, 32 bytes of parents
+        assert refused(at, lead=2, lead_stride=8000)
+    # every place next to rows with gaps
+    g = np.random.default_rng(0)
+    for _ in range(60):
+        row, span, strides = int(g.integers(1, 40)), 0, {}
+        sizes = dict(inner=int(g.integers(1, 4)), lead=int(g.integers(2, 4)), b=2, slot=4)
+        span = row
+        for name in g.permutation(list(sizes)):
+            strides[str(name)] = span + int(g.integers(0, 90))
+            span += strides[str(name)] * (sizes[str(name)] - 1)
+        v = dict(inner=sizes["inner"], lead=sizes["lead"], row_bytes=row, **{f"{k}_stride": x for k, x in strides.items()})
+        held = np.zeros(span + 128, bool)
+        for i in np.ndindex(*sizes.values()):
+            at = 64 + sum(n * strides[k] for n, k in zip(i, sizes))
+            held[at:at + row] = True
+        for at in range(24, len(held) - 32, 4):
+            assert refused(FAKE + at - 64, **v) == bool(held[at:at + 32].any())
+
+
 def a_cache(**over):
     from paper_2506_00185_amd.tokens import _Cache
     c = _Cache(struct_size=C.sizeof(_Cache), format=0, n_pages=10, page_size=16, heads=2, dim=64, k=FAKE, v=FAKE, k_exp=FAKE, v_exp=FAKE, table=FAKE,
