@@ -416,7 +416,8 @@ int rnnt_cache_read(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_
  * A node whose parent is neither -1 nor a node before it is padding: its output, and that of nodes below it, is zero, its rows need not
  * have been written.  A query that sees nothing gets zeros; one that sees a row of NaN, or is not finite itself, NaN.  Rows that a query does not see
  * have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; logits are taken as
- * within 1e30, the value rows of a sequence's head, those of zeros aside, as within 2^100 of the first 64 of them.  Outputs repeat bit for bit.
+ * within 1e30, the exponents s of a sequence's head's value rows, those of zeros aside, as within 45 of the first one's (looked for among 64 tokens, padding
+ * aside; none there: 0).  Outputs repeat bit for bit.
  */
 typedef struct {
   uint32_t struct_size;

@@ -41,6 +41,10 @@ constexpr int kTreeMax = 1024;  // nodes of a tree with parents
 constexpr float kMStart = -1e30f;
 constexpr float kTop = 7.f;   // P' of the running maximum is 2^kTop
 constexpr float kSlack = 8.f;
+// Value exponents are relative to the head's first row's (reference_exp), and those of rows of zeros, which could be any, the lowest for which the range of
+// float32 holds: with rows up to 2^45 on either side, of two that weigh alike the smaller's P' is 2^-90 of the larger's, which leaves 36 bits above 2^-126
+// for what weighs less.
+constexpr int kZeroRow = -45;
 
 __device__ __forceinline__ uint32_t perm_b32(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
 __device__ __forceinline__ uint32_t e4m3_lo(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.f, false)); }
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
       }
       wave_lds_order();
       if (__any(lane >= 32 && head.there && head.e == kExpZero)) {
-        // maybe a row of zeros, whose exponent says nothing about the others' and must not become the largest: 16 lanes hold its words
+        // maybe a row of zeros, whose P' must not push those of smaller rows beyond float16's range, since it adds nothing: 16 lanes hold its words
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           uint32_t any = 0;
@@ -368,8 +372,8 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
           const uint64_t held = __ballot(any != 0);
           const int t = (j >> 2) * 16 + 4 * g4 + (j & 3);
           if (l16 == 0 && !(held >> (16 * g4) & 0xffff) && fabsf(mt.v_exp[t]) < INFINITY) {
-            mt.v_exp[t] = 0.f;
-            mt.v_inv[t] = 1.f;
+            mt.v_exp[t] = (float)kZeroRow;
+            mt.v_inv[t] = 0x1p45f;
           }
         }
         wave_lds_order();

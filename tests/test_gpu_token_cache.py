@@ -571,6 +571,53 @@ def test_sizes_of_keys_values_and_queries(fmt, size):
         check(cache, table, cuda(q * 30, torch.float32), np.array([149, 20]))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("length", [20, 700])
+def test_value_rows_of_far_apart_sizes(fmt, length):
+    """Exponents up to 45 on either side of that of the head's first row, side by side and beside rows of zeros; the first row itself weighs nothing, or
+    as much as they do.
+
+    To tolerance() a row of zeros adds what its own probability leaves of the others: the largest P' is at least 2^7 and a sum of two float16 is off by up to
+    2^-25, the last half step of the second, so by 2^-32 of the largest.  Where that is a row of zeros', of weight w <= 1, it stands for w 2^(s - 45), s the first
+    row's exponent, and 2^s times the largest y, which the others' errors are multiplied by, is at most twice the first row's largest |v|:
+    2^-32 2^-45 2 max|v| = 2^-76 max|v| for each token."""
+    import torch
+    from paper_2506_00185_amd import KVCache
+    g = np.random.default_rng(length)
+    table, n_pages = pages(g, 1, -(-length // 16))
+    table, cache = cuda(table), KVCache(n_pages, 16, 1, 64, fmt)
+    zero = cuda(np.zeros(1, np.int32))
+    q = torch.zeros(1, 1, 2, 64, device="cuda")
+    q[..., 0], q[:, :, 1, 0] = 1.0, 0.5
+
+    def near(q, kept, parents, scale, most):
+        tokens = kept + len(parents[0])
+        k, v = values_of(cache, table, tokens)
+        want, size, far = R.attend(q.double().cpu().numpy(), k, v, [kept], parents, scale)
+        y = cache.attend(q, table, cuda(np.array([kept], np.int32)), cuda(np.array(parents, np.int32)), scale).double().cpu().numpy()
+        assert (np.abs(y - want) <= tolerance(want, size, far, "f32", 64, tokens) + tokens * 2.0**-76 * most).all()
+
+    for sizes in ([45, -45], [-45, None], [45, None], [-45], [45], [None], [45, 0, -45, None], [45, -20, None]):
+        for first in (-150.0, 1.0):
+            v = g.standard_normal((1, length, 1, 64))
+            v /= np.abs(v).max(-1, keepdims=True)  # of one exponent
+            x = np.full(length, -300.0)
+            x[0] = first
+            for i, t in enumerate(np.sort(g.permutation(np.arange(1, length))[:3 * len(sizes)])):
+                size, x[t] = sizes[i % len(sizes)], g.uniform(-3, 3)
+                v[0, t] *= 0.0 if size is None else 2.0**size
+            k = np.zeros((1, length, 1, 64))
+            k[0, :, 0, 0] = x
+            cache.write(cuda(k, torch.float32), cuda(v, torch.float32), table, zero)
+            near(q, length - 1, [[-1]], 1.0, 1.0)
+    # the first row is a node that the others do not see
+    v = g.standard_normal((1, 6, 1, 64))
+    v = v / np.abs(v).max(-1, keepdims=True) * 2.0 ** np.array([45, 0, -3, 0, 1, 0])[:, None, None]
+    v[0, 3] = 0
+    cache.write(cuda(0.1 * g.standard_normal((1, 6, 1, 64)), torch.float32), cuda(v, torch.float32), table, zero)
+    near(cuda(g.standard_normal((1, 6, 2, 64)), torch.float32), 0, [[-1, -1, 1, 2, 3, 1]], 0.125, 2.0**45)
+
+
 def test_logits_that_rise_along_the_sequence():
     """The running maximum moves at every tile, by little and by much."""
     import torch
