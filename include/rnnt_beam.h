@@ -414,8 +414,8 @@ int rnnt_cache_read(const rnnt_cache_t *cache, const rnnt_rows_t *k, const rnnt_
  * parents[b, i], a node before it or -1; a query sees its node and the node's ancestors.  parents NULL: a chain, node i's parent is i - 1
  * (one token, or a chunk).  Queries are the last n nodes (n = tree: all; fewer where rows of earlier nodes are in the cache but not asked for).
  * A node whose parent is neither -1 nor a node before it is padding: its output, and that of nodes below it, is zero, its rows need not
- * have been written.  A query that sees nothing gets zeros; one that sees a row of NaN, or is not finite itself, NaN.  Rows that a query does not see
- * have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; logits are taken as
+ * have been written.  A query that sees nothing gets zeros; one that sees a row of NaN, or is not finite itself, NaN.  (In arrays that the caller filled: y of NaN
+ * make their row one of NaN, among the values infinite ones too.)  Rows that a query does not see have no effect on it, whatever they hold.  Query head j reads key head j / (q_heads / heads).  Sums and soft-max are float32; logits are taken as
  * within 1e30, the exponents s of a sequence's head's value rows, those of zeros aside, as within 45 of the first one's (looked for among 64 tokens, padding
  * aside; none there: 0).  Outputs repeat bit for bit.
  */

@@ -87,6 +87,12 @@ __device__ __forceinline__ uint32_t finite_f16(uint32_t w) {
   return (w & 0x7c000000u) == 0x7c000000u ? w & 0xffffu : w;
 }
 
+// whether one of a word's four e4m3 values, or of its two float16, is NaN or infinite: not zero
+template <int FMT>
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w) {
+  return FMT == 8 ? ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+}
+
 // the N bytes at p (N = 4, 8, 16, 32, 64), or zeros
 template <int N>
 struct Bytes {
@@ -379,6 +385,23 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
         wave_lds_order();
       }
     }
+    // Values that are not finite, in arrays that the caller filled, make their row one of NaN.  Where all rows are seen they reach the sums by
+    // themselves; elsewhere they must not meet the p of zero of a query that does not see them, nor may what rows that are not there hold.
+    bool odd = false;
+    if (careful) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int w = 0; w < VN * FB / 4; ++w) any |= odd_codes<FMT>(values[j].w[w]);
+        const uint64_t held = __ballot(any != 0);
+        if (!held) continue;
+        odd = true;
+        const int t = (j >> 2) * 16 + 4 * g4 + (j & 3);
+        if (l16 == 0 && (held >> (16 * g4) & 0xffff) && fabsf(mt.v_exp[t]) < INFINITY) mt.v_exp[t] = NAN;
+      }
+      if (odd) wave_lds_order();
+    }
     floatx4 ks[2], ve[2], vi[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -467,7 +490,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
           va[1][jp] = perm_b32(hi, lo, 0x07060302u);
         }
       }
-      if (careful) {  // rows of padding, or of nodes that no query sees, hold anything: a p of zero must not meet a NaN or an infinity
+      if (odd) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -527,8 +550,11 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = fmaf(f, sh.o[w][r][d + j], o[j]);
     }
+    // (a row's DP / 4 lanes: all of its values are NaN if one of the rows it sees has one that is not finite)
+    const bool finite = fabsf(o[0]) < INFINITY && fabsf(o[1]) < INFINITY && fabsf(o[2]) < INFINITY && fabsf(o[3]) < INFINITY;
+    const uint64_t others = ~0ull >> (64 - DP / 4) << (lane & ~(DP / 4 - 1));
     const bool gone = treed && sh.gone[r], none = gone || l == 0.f;
-    const float inv = 1.f / l, back = ldexpf(1.f, e0 - 127);
+    const float inv = __ballot(!finite) & others ? NAN : 1.f / l, back = ldexpf(1.f, e0 - 127);
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = none ? 0.f : o[j] * inv * back;
     if (a.splits > 1 && d == 0) a.stat[part_row + row] = make_float2(m_all, gone ? -1.f : l);

@@ -474,6 +474,44 @@ def test_rows_that_a_query_does_not_see_do_not_matter(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+def test_codes_that_are_not_finite(fmt, dim):
+    """In arrays of the caller's: such a code among the values makes its row one of NaN, wherever it stands, for the queries that see it and for no others; a NaN
+    among the keys does too."""
+    import torch
+    g = np.random.default_rng(dim)
+    lens, n = np.array([300, 300]), 5
+    cache, table = filled(g, 2, 310, 2, dim, fmt, 16)
+    parents = np.array([[-1, 0, 0, 1, 2]] * 2)
+    q = cuda(g.standard_normal((2, n, 6, dim)), torch.float32)
+    d_lens, d_parents = cuda(lens.astype(np.int32)), cuda(parents.astype(np.int32))
+    clean, alone = cache.attend(q, table, d_lens, d_parents), cache.attend(q, table, d_lens, d_parents, max_len=1)
+    codes = [0x7F, 0xFF] if fmt == "e4m3" else [0x7E00, 0x7C00, 0xFC00]
+    for t in (cache.k, cache.v):
+        raw = t.view(torch.uint8 if fmt == "e4m3" else torch.int16)
+        for code in codes if t is cache.v else codes[:1]:
+            code = code - 0x10000 if code > 0x7FFF else code
+            for at in (0, 40, 290, 299, 302, 304):  # tiles of the past, the last of them, nodes
+                for x in {0, dim // 2 + 1, dim - 1}:
+                    place = int(table[1, at // 16]), 1, at % 16, x
+                    kept = raw[place].clone()
+                    raw[place] = code
+                    sees = torch.tensor([at < 300 or (at - 300) in R.path_of(list(parents[1]), i) for i in range(n)])
+                    for bound, want in ((None, clean), (1, alone)):
+                        got = cache.attend(q, table, d_lens, d_parents, max_len=bound)
+                        assert torch.equal(got[0], want[0]) and torch.equal(got[1, :, :3], want[1, :, :3])
+                        assert torch.equal(got[1, ~sees, 3:], want[1, ~sees, 3:]), (at, x)
+                        assert torch.isnan(got[1, sees, 3:]).all(), (at, x)
+                    raw[place] = kept
+    # a node that is not there reads the first row of all, whatever it holds
+    cache.v.view(torch.uint8)[0, 0, 0] = 0x7F if fmt == "e4m3" else 0x7E
+    first = (table == 0).nonzero()
+    holes = torch.where(table == 0, -1, table)
+    if len(first):
+        assert torch.isfinite(cache.attend(q, holes, d_lens, d_parents)).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("kept", [0, 3])
 def test_padding_ahead_of_the_nodes(fmt, kept):
     """The first rows that a sequence has are padding's, and those of nodes below it, which hold anything; the tokens kept before are zeros."""
