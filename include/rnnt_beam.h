@@ -427,7 +427,7 @@ typedef struct {
   float scale;
   int32_t max_len;             /* host's bound of lens + tree, by which the work is split: a smaller one than the lengths only costs time */
   rnnt_rows_t q;               /* [B, n, q_heads, dim] */
-  void *out;                   /* [B, n, q_heads, dim], contiguous */
+  void *out;                   /* [B, n, q_heads, dim], contiguous, at any address of its type; does not overlap q */
   const int32_t *lens;         /* [B] */
   const int32_t *parents;      /* [B, tree] or NULL */
   void *workspace;             /* of rnnt_cache_attend_workspace bytes, 16-byte aligned; as that of rnnt_select_t */

@@ -119,9 +119,16 @@ __device__ __forceinline__ void load_bytes(Bytes<N> &d, const char *p) {
 __device__ __forceinline__ int64_t out_row(const AttendArgs &a, int b, int h, int row) {
   return (((int64_t)b * a.n + row / a.group) * (a.c.heads * a.group) + h * a.group + row % a.group) * a.c.dim;
 }
-__device__ __forceinline__ void put_output(float *p, floatx4 o) { *reinterpret_cast<floatx4 *>(p) = o; }
-__device__ __forceinline__ void put_output(_Float16 *p, floatx4 o) { *reinterpret_cast<uintx2_t *>(p) = uintx2_t{pack_f16(o[0], o[1]), pack_f16(o[2], o[3])}; }
-__device__ __forceinline__ void put_output(uint16_t *p, floatx4 o) { *reinterpret_cast<uintx2_t *>(p) = uintx2_t{pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])}; }
+// (from any address of their type: the hardware takes such stores whole)
+__device__ __forceinline__ void put_output(float *p, floatx4 o) { __builtin_memcpy(p, &o, 16); }
+__device__ __forceinline__ void put_output(_Float16 *p, floatx4 o) {
+  const uint32_t w[2] = {pack_f16(o[0], o[1]), pack_f16(o[2], o[3])};
+  __builtin_memcpy(p, w, 8);
+}
+__device__ __forceinline__ void put_output(uint16_t *p, floatx4 o) {
+  const uint32_t w[2] = {pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])};
+  __builtin_memcpy(p, w, 8);
+}
 
 // blocks of four waves that a compute unit holds, one wave of each on a SIMD: what the registers allow
 constexpr int attend_blocks(int fmt, int dp, int mt) { return mt > 1 ? 2 : dp == 64 ? 4 : dp == 128 && fmt == 8 ? 3 : 2; }

@@ -692,6 +692,23 @@ def test_strided_queries_streams_and_out():
         assert torch.equal(out, a)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_outputs_and_rows_that_start_anywhere(dtype):
+    """From any element on, with one split of the tokens and with several; what lies next to them stays."""
+    import torch
+    g = np.random.default_rng(22)
+    t = R.torch_type(dtype)
+    for length in (30, 900):
+        cache, table = filled(g, 2, length + 3, 2, 80, "f16", 16)
+        q, lens = cuda(g.standard_normal((2, 3, 4, 80)), t), cuda(np.array([length, length // 2], np.int32))
+        want = cache.attend(q, table, lens)
+        for off in (1, 2, 3, 5):
+            room = torch.full((want.numel() + 8,), 7.0, dtype=t, device="cuda")
+            out = room[off:off + want.numel()].view(want.shape)
+            cache.attend(q, table, lens, out=out)
+            assert torch.equal(out, want) and (room[:off] == 7).all() and (room[off + want.numel():] == 7).all()
+
+
 def test_two_streams_at_once():
     """Calls that overlap have a workspace each."""
     import torch
