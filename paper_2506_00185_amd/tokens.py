@@ -124,14 +124,16 @@ def _enter(T, t, stream, inputs):
     if stream is None and index == T.device_of():
         return C.c_void_p(T.raw_stream(index)), None
     import torch
-    scope = contextlib.ExitStack()
-    scope.enter_context(torch.cuda.device(index))
-    if stream is not None and stream != torch.cuda.current_stream(index):
-        _refuse(stream.device == t.device, f"the stream is of {stream.device}, the tensors are on {t.device}")
-        for x in inputs:  # of another stream: not to be given away before this call has used them
-            if x is not None:
-                x.record_stream(stream)
-        scope.enter_context(torch.cuda.stream(stream))
+    with contextlib.ExitStack() as stack:  # (closed here only if something below is refused)
+        stack.enter_context(torch.cuda.device(index))
+        if stream is not None and stream != torch.cuda.current_stream(index):
+            _refuse(stream.device == t.device, f"the stream is of {stream.device}, the tensors are on {t.device}")
+            for x in inputs:  # of another stream: not to be given away before this call has used them
+                if x is not None:
+                    _refuse(x.device == t.device, f"a tensor is on {x.device}, not on {t.device}")
+                    x.record_stream(stream)
+            stack.enter_context(torch.cuda.stream(stream))
+        scope = stack.pop_all()
     return C.c_void_p((stream or torch.cuda.current_stream(index)).cuda_stream), scope
 
 

@@ -349,6 +349,46 @@ def test_prefix_trees_of_other_integers():
         nbest_tree(tokens, lens + 2**30)
 
 
+def test_the_current_device_comes_back_when_a_stream_or_an_input_is_refused(monkeypatch):
+    """Without a GPU: the device's and the stream's scopes are stand-ins that write down when they are entered and left."""
+    import contextlib
+    from types import SimpleNamespace
+    import torch
+    from paper_2506_00185_amd import RnntBeamError, tokens
+    log = []
+
+    @contextlib.contextmanager
+    def scope(what):
+        log.append(("in", what))
+        try:
+            yield
+        finally:
+            log.append(("out", what))
+
+    def tensor(device, fails=False):
+        def record_stream(stream):
+            if fails:
+                raise RuntimeError("no")
+        device = torch.device(device)
+        return SimpleNamespace(is_cuda=device.type == "cuda", get_device=lambda: device.index, device=device, record_stream=record_stream)
+
+    monkeypatch.setattr(torch.cuda, "device", lambda i: scope(f"device {i}"))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: scope("stream"))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda i: SimpleNamespace(device=torch.device("cuda", i), cuda_stream=0))
+    T = SimpleNamespace(device_of=lambda: 0)
+    mine, other = (SimpleNamespace(device=torch.device("cuda", i), cuda_stream=7) for i in (1, 0))
+    here = tensor("cuda:1")
+    for stream, inputs, error in [(other, [here], RnntBeamError), (mine, [here, None, tensor("cpu")], RnntBeamError), (mine, [here, tensor("cuda:0")], RnntBeamError),
+                                  (mine, [here, tensor("cuda:1", fails=True)], RuntimeError)]:
+        with pytest.raises(error):
+            tokens._enter(T, here, stream, inputs)
+        assert sorted(w for e, w in log if e == "in") == sorted(w for e, w in log if e == "out"), log
+    raw, close = tokens._enter(T, here, mine, [here, None])
+    assert raw.value == 7 and log[-2:] == [("in", "device 1"), ("in", "stream")]
+    close.close()
+    assert log[-2:] == [("out", "stream"), ("out", "device 1")]
+
+
 # ---------------------------------------------------------------- the plain implementations themselves
 def test_plain_formats():
     import torch
