@@ -8,22 +8,25 @@ namespace rb {
 // ---- soft-max statistics in float64
 // The keys of an utterance's hypotheses are compared with each other, and the sums of rows decide between candidates whose logits differ by
 // little: float32 exponentials leave 1e-8 to 1e-7 of a row's log sum open.  float64 multiply-adds run at the rate of float32 ones here, so
-// the exponential is a polynomial in float64: e^d = 2^n e^f with n = d / ln 2 rounded, and for e^f the polynomial of degree 7 through the
-// Chebyshev points of [-ln 2 / 2, ln 2 / 2], off by at most 5.5e-11 of its value.  Of float64 only sums and multiply-adds run at that rate: n is
+// the exponential is a polynomial in float64: e^d = 2^n e^f with n = d / ln 2 rounded, and for e^f the polynomial of degree 10 through the
+// Chebyshev points of [-ln 2 / 2, ln 2 / 2], off by at most 3.3e-16 of its value, three half steps of float64 (degree 7 would leave 5.5e-11, and keys
+// off by 1e-12; 128 x 10 x 8192 logits take 20.3 us for 19.4).  Of float64 only sums and multiply-adds run at that rate: n is
 // read from the last bits of d / ln 2 + 1.5 2^52 and added to the exponent of e^f, in place of instructions that round, convert and scale.
-// (Sums that are brought to a common reference are multiplied by the library's exp, or that error would count again.)
 __device__ __forceinline__ double exp_d(double d) {  // d up to 700
   constexpr double kRound = 6755399441055744.;
   d = fmax(d, -690.);  // (of -inf too: e^-690 is nothing beside the 1 of the largest)
   const double s = fma(d, kLog2E, kRound), f = fma(s - kRound, -0.6931471805599453, d);
-  double p = 0.00019907569324365478;
-  p = fma(p, f, 0.0013948578338419519);
-  p = fma(p, f, 0.008333283538688176);
-  p = fma(p, f, 0.0416662183191124);
-  p = fma(p, f, 0.1666666678630866);
-  p = fma(p, f, 0.500000010772923);
-  p = fma(p, f, 0.999999999995509);
-  p = fma(p, f, 0.9999999999595617);
+  double p = 2.7626357241447223e-07;
+  p = fma(p, f, 2.764018079620985e-06);
+  p = fma(p, f, 2.4801504346997686e-05);
+  p = fma(p, f, 0.00019841170270440067);
+  p = fma(p, f, 0.0013888888932488599);
+  p = fma(p, f, 0.008333333385667782);
+  p = fma(p, f, 0.04166666666657314);
+  p = fma(p, f, 0.16666666666554406);
+  p = fma(p, f, 0.5000000000000006);
+  p = fma(p, f, 1.0000000000000067);
+  p = fma(p, f, 1.0);
   return __hiloint2double(__double2hiint(p) + (__double2loint(s) << 20), __double2loint(p));
 }
 

@@ -75,6 +75,23 @@ def test_finished_hypotheses_and_empty_slots(K, V):
     assert np.isneginf(s).all() and (p == -1).all() and (t == -3).all() and not d.any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("B,K,V", [(4, 4, 1024), (3, 16, 900), (1, 1, 16000), (2, 10, 8192), (1, 12, 32003), (3, 5, 12345)])
+def test_keys_have_the_bits_of_float64(B, K, V, dtype):
+    """Against 64-bit mantissas.  The sum is off by the polynomial's 3.3e-16, four half steps of its evaluation, n times what ln 2 in float64 leaves of it (2.4e-17,
+    n up to 145 for terms of e^-100, what is below weighs nothing) and up to 64 additions of a lane and 16 of lanes and parts: 1.3e-14.  Three more
+    roundings, of numbers below 64."""
+    logits, scores = make(B, K, V, dtype, 3 * B + K + V)
+    x = logits.double().cpu().numpy().astype(np.longdouble)
+    assert np.finfo(np.longdouble).nmant >= 63
+    top = x.max(-1, keepdims=True)
+    keys = scores.astype(np.longdouble)[..., None] + (x - (top + np.log(np.exp(x - top).sum(-1, keepdims=True))))
+    got = run(logits, scores)
+    assert np.abs(got[0]).max() < 64 and np.abs(x).max() < 64
+    there = np.take_along_axis(keys.reshape(B, -1), got[1].astype(np.int64) * V + got[2], 1)
+    assert np.abs(got[0] - there).max() <= 1.3e-14 + 3 * 64 * 2.0**-53
+
+
 def run_in(fill, logits, scores, done=None, eos=-1):
     """The C call with a workspace of the caller's that holds ``fill`` in every byte."""
     import ctypes as C
