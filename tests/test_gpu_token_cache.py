@@ -709,6 +709,37 @@ def test_outputs_and_rows_that_start_anywhere(dtype):
             assert torch.equal(out, want) and (room[:off] == 7).all() and (room[off + want.numel():] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,n,treed", [(64, 1, False), (80, 5, True), (128, 1, False), (128, 70, True), (256, 3, True)])
+def test_what_a_workspace_held_does_not_matter(dim, n, treed, dtype):
+    """The C call with a workspace of the caller's that holds zeros, numbers or NaN; sequences that fill some of its splits, or one, or have nothing."""
+    import ctypes as C
+    import torch
+    from paper_2506_00185_amd import load_library
+    from paper_2506_00185_amd.tokens import _Attend, _Rows, _torch
+    lib, g = load_library(), np.random.default_rng(dim + n)
+    lens = np.array([3000, 700, 3, 0])
+    cache, table = filled(g, 4, 3000 + n, 2, dim, "e4m3", 16)
+    q = cuda(g.standard_normal((4, n, 4, dim)), R.torch_type(dtype))
+    parents = some_tree(g, 4, n) if treed else None
+    table[3] = -1  # no page at all
+    want = cache.attend(q, table, cuda(lens.astype(np.int32)), None if parents is None else cuda(parents.astype(np.int32)))
+    assert torch.isfinite(want).all() and want[0].any()
+    c = cache._view(_torch(), table, 4)
+    d_lens, d_parents = cuda(lens.astype(np.int32)), None if parents is None else cuda(parents.astype(np.int32))
+    out = torch.empty_like(q)
+    a = _Attend(C.sizeof(_Attend), TYPES.index(dtype), 4, n, n, 4, dim**-0.5, table.shape[1] * 16, _Rows(q.data_ptr(), *q.stride()[:3]), out.data_ptr(),
+                d_lens.data_ptr(), None if parents is None else d_parents.data_ptr())
+    need = lib.rnnt_cache_attend_workspace(C.byref(c), C.byref(a))
+    assert need > 0
+    for fill in (0x00, 0x40, 0x7f, 0xbf, 0xff):
+        work = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = work.data_ptr(), need
+        out.fill_(7.0)
+        assert lib.rnnt_cache_attend(C.byref(c), C.byref(a), C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+        assert torch.equal(out, want)
+
+
 def test_two_streams_at_once():
     """Calls that overlap have a workspace each."""
     import torch
