@@ -331,7 +331,7 @@ int rnnt_beam_kernel_times(rnnt_beam_t *h, const char **names, float *ms, int32_
  * and move the states of hypotheses.  All pointers are memory of the current device unless stated; work is enqueued on hip_stream and the calls return at
  * once; nothing is allocated, no call waits, all may be captured into a HIP graph.  Structures are plain data, versioned by struct_size;
  * strides count elements (of rnnt_states_t: bytes).  RNNT_E_ARG with a message (rnnt_beam_last_error(NULL), of this thread) for what the host
- * can see to be wrong; what only the device sees (tables, lengths, parents, counts) is taken as described at each call, never beyond the arrays.
+ * can see to be wrong, batches of none among it; what only the device sees (tables, lengths, parents, counts) is taken as described at each call, never beyond the arrays.
  */
 typedef enum { RNNT_TYPE_F32 = 0, RNNT_TYPE_F16 = 1, RNNT_TYPE_BF16 = 2 } rnnt_type_t;
 

@@ -110,16 +110,16 @@ int attend_plan(const CacheView &c, bool f8, const rnnt_attend_t *s, AttendPlan 
   p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
   // Two tiles of rows for a block: a token's key and value are loaded and unpacked once for both, but half as many waves fit.  That pays where
   // blocks of one tile would fill the chip, and where a row is more than 64 bytes (trees of 61 nodes over 500 to 2000 tokens, microseconds with
-  // one tile and two: 16 sequences x 32 heads on 8 of 128, float32 on a cache of 16 bits 133 and 88, bfloat16 on e4m3 84 and 64; of 64 on 16
-  // bits 75 and 55, on e4m3 46 and 44, but 24 and 24 with 8 sequences x 16 heads, and 57 and 67 for 2 chunks of 2000; 2 sequences x 8 heads of 128: 20 and 23).
+  // one tile and two: 16 sequences x 32 heads on 8 of 128, float32 on a cache of 16 bits 131 and 85, bfloat16 on e4m3 86 and 72; of 64 on 16
+  // bits 77 and 55, on e4m3 50 and 48, but 25 and 26 with 8 sequences x 16 heads, and 58 and 72 for 2 chunks of 2000; 2 sequences x 8 heads of 128: 21 and 22).
   // With 256 dims the sums of two tiles do not fit the registers.
   const int64_t tiles = (rows + 15) / 16;
   p.mt = tiles > 1 && pairs * tiles > kUnits && (f8 ? p.dp == 128 : p.dp < 256) ? 2 : 1;
   p.row_tiles = (int)((rows + 16 * p.mt - 1) / (16 * p.mt));
   // Splits of equal length for all sequences, so that short ones leave no long ones behind: enough blocks for two on every unit, four where a
-  // unit holds three or more (32 sequences of 1000 to 8000 tokens, 32 heads on 8 of 128: 75 us with two, 65 with four, 70 with six; where it holds two, four
+  // unit holds three or more (32 sequences of 1000 to 8000 tokens, 32 heads on 8 of 128: 76 us with two, 66 with four, 71 with six; where it holds two, four
   // cost: 16 trees of 61 nodes 64 us for 51), none shorter than 256 tokens, two tiles for each of its waves (one sequence of 8000 tokens:
-  // 15.7 us from 128 tokens on, 12.7 from 256, 14.2 from 512).
+  // 16.0 us from 128 tokens on, 13.1 from 256, 14.5 from 512).
   const int64_t room = (int64_t)c.width << c.page_shift, longest = s->max_len < room ? (s->max_len > 1 ? s->max_len : 1) : room;
   const int64_t others = pairs * p.row_tiles, want = ((attend_blocks(f8 ? 8 : 16, p.dp, p.mt) > 2 ? 4 : 2) * kUnits + others - 1) / others, most = (longest + 255) / 256;
   int64_t splits = want < most ? want : most;
@@ -128,7 +128,7 @@ int attend_plan(const CacheView &c, bool f8, const rnnt_attend_t *s, AttendPlan 
   p.splits = (int)splits;
   p.split_len = (int)len;
   p.blocks = (pairs * splits + 7) / 8 * 8 * p.row_tiles;
-  p.join_shares = 1;  // four splits for each thread of the join (one sequence of 8000 tokens: 12.7 us, with all splits on one thread 15.6)
+  p.join_shares = 1;  // four splits for each thread of the join (one sequence of 8000 tokens: 13.1 us, with all splits on one thread 16.3)
   while (p.join_shares < 8 && p.join_shares * 4 < splits && c.dim / 4 * p.join_shares * 2 <= 256) p.join_shares *= 2;
   p.workspace = splits > 1 ? splits * pairs * rows * (int64_t)(c.dim * sizeof(float) + sizeof(float2)) : 0;
   return RNNT_OK;

@@ -10,8 +10,8 @@ using namespace rb;
 
 namespace {
 
-// Logits of an utterance that k_select_one takes in one tile per wave.  Up to there one launch is faster than two: 4 x 1024 7.4 us and 8.5,
-// 32 x 8 x 2048 11.9 and 12.2; twice as many would take its 16 waves two tiles each, one after the other.
+// Logits of an utterance that k_select_one takes in one tile per wave.  Up to there one launch is faster than two: 4 x 1024 7.5 us and 8.7,
+// 32 x 8 x 2048 12.2 and 12.3; twice as many would take its 16 waves two tiles each, one after the other.
 constexpr int kSelOneMax = 16 * 64 * 16;
 
 // Parts of a row.  In one launch 16 / beam waves share a row; in two, blocks of up to 8192 logits, a tile for their four waves, as many as the
@@ -29,8 +29,8 @@ SelectPlan select_plan(int B, int beam, int V) {
     return p;
   }
   const int most = kSelLists / beam;
-  // a chip's worth of blocks, of 1024 to 8192 logits each (10 x 8192: 10.7 us, with blocks of 8192 alone 11.3; for twice as many blocks
-  // 128 x 10 x 8192 would take 22.3 us for 19.4)
+  // a chip's worth of blocks, of 1024 to 8192 logits each (10 x 8192: 10.8 us, with blocks of 8192 alone 11.5; for twice as many blocks
+  // 128 x 10 x 8192 would take 23.5 us for 20.4)
   const int64_t rows = (int64_t)B * beam;
   int64_t parts = (V + 8191) / 8192;
   const int64_t fill = (1024 + rows - 1) / rows, fine = (V + 1023) / 1024;
@@ -42,8 +42,8 @@ SelectPlan select_plan(int B, int beam, int V) {
 
 template <typename TT>
 int select_typed(const SelectArgs &a, bool one, hipStream_t stream) {
-  // tiles no longer than the parts need: what a tile has beyond a part costs as much as what it has in it (10 x 8192 in parts of 1024: 10.7 us,
-  // with tiles of 8192 16.1; long parts in tiles of 4096: 128 x 10 x 8192 21.6 us for 19.4)
+  // tiles no longer than the parts need: what a tile has beyond a part costs as much as what it has in it (10 x 8192 in parts of 1024: 10.8 us,
+  // with tiles of 8192 16.5; long parts in tiles of 4096: 128 x 10 x 8192 23.0 us for 20.4)
   constexpr int kVec = 16 / (int)sizeof(typename TT::T);
   if (one) {
     const int vecs = (a.part_len + 64 * kVec - 1) / (64 * kVec);

@@ -19,10 +19,11 @@ namespace rb {
 // types: with one, whose 11 bits are less than float32 keeps, outputs in bfloat16 were rounded to a neighbour now and then; sums are float32.
 // M follows the running maximum only when a logit passes it by 2^8 (the range that float16 leaves above), so that the accumulators are
 // multiplied by a correction a few times in a row of thousands of tokens.
-// Measured: one token for each of 32 sequences of 1000 to 8000, 32 heads on 8 of 128 in e4m3: 61 us and 4 for the join, 4.6 TB/s of a large copy's
-// 5.3; bound by memory, a block's beginning (three dependent loads, 5 us) and the lengths' spread are the rest.  61 nodes for each of 16 sequences, 500 to 2000 tokens, float32 on
-// a cache of 16 bits: 51 us, 180 TFLOP/s of products, bound by instructions: for a tile of 32 tokens and 32 rows a wave issues 64 products and
-// some 350 vector instructions.  One sequence of 187 tokens: 7 us, a chain of loads.
+// Measured: one token for each of 32 sequences of 1000 to 8000, 32 heads on 8 of 128 in e4m3: 62 us and 4 for the join, 4.5 TB/s of a large copy's
+// 5.3; bound by memory, a block's beginning (three dependent loads, 5 us) and the lengths' spread are the rest.  61 nodes for each of 16 sequences of 400 to 1900 tokens,
+// 16 heads on 4 of 128, float32 on a cache of 16 bits: 51 us, 180 TFLOP/s of products: for a tile of 32 tokens and 32 rows a wave issues 64 products and
+// some 350 vector instructions, half of the 5 000 cycles that a tile takes with two waves on a SIMD; the other half are waits, and a block's beginning
+// and end, 17 000 and 6 000 cycles.  One sequence of 187 tokens: 7 us, a chain of loads.
 struct AttendArgs {
   CacheView c;
   const void *q;

@@ -10,7 +10,7 @@ namespace rb {
 // little: float32 exponentials leave 1e-8 to 1e-7 of a row's log sum open.  float64 multiply-adds run at the rate of float32 ones here, so
 // the exponential is a polynomial in float64: e^d = 2^n e^f with n = d / ln 2 rounded, and for e^f the polynomial of degree 10 through the
 // Chebyshev points of [-ln 2 / 2, ln 2 / 2], off by at most 3.3e-16 of its value, three half steps of float64 (degree 7 would leave 5.5e-11, and keys
-// off by 1e-12; 128 x 10 x 8192 logits take 20.3 us for 19.4).  Of float64 only sums and multiply-adds run at that rate: n is
+// off by 1e-12 to 2e-11; 128 x 10 x 8192 logits take 20.3 us for 19.4).  Of float64 only sums and multiply-adds run at that rate: n is
 // read from the last bits of d / ln 2 + 1.5 2^52 and added to the exponent of e^f, in place of instructions that round, convert and scale.
 __device__ __forceinline__ double exp_d(double d) {  // d up to 700
   constexpr double kRound = 6755399441055744.;
@@ -363,9 +363,9 @@ __global__ __launch_bounds__(1024) void k_select_one(SelectArgs a) {
 // ---- many blocks for a row: each leaves the best of its part, a second launch joins them.  A block's four waves take tiles of 256 E logits
 // together: a bound that the `beam` best of a tile reach is the beam-th largest of the maxima of 32 groups of 8 lanes; of the logits
 // that reach it and what earlier tiles left, rarely more than twice `beam`, one wave takes the best.
-// Measured: 128 x 10 x 8192 logits of 16 bits in 14 us (read at 5.3 TB/s they would take 4), 32 x 12 x 32003 of 32, a fifth of the rows finished, in 18 (7.4).  Of the 14 some 4 go
-// into the float64 exponentials (16 instructions for a logit), 3 each into the first loads, which all blocks wait for at once, and into finding
-// and ranking the candidates.  Five blocks share a unit: what keeps the registers to 96, with 80 some are spilt and it takes 15.7 us.
+// Measured: 128 x 10 x 8192 logits of 16 bits in 15 us (read at 5.3 TB/s they would take 4), 32 x 12 x 32003 of 32, a fifth of the rows finished, in 19 (7.4).  Of the 15 some 5 go
+// into the float64 exponentials (19 instructions for a logit), 3 each into the first loads, which all blocks wait for at once, and into finding
+// and ranking the candidates.  Five blocks share a unit: what keeps the registers to 96, with 80 some are spilt, which costs 1.7.
 struct SelScan {
   float group[32];
   GroupKeys group_key;
@@ -508,9 +508,9 @@ static __global__ __launch_bounds__(64) void k_select_join(SelectArgs a) {
 }
 
 // ---- states of hypotheses to the slots of their successors, in place: state[b, k] = state[b, parent[b, k]]
-// A thread reads its column of all slots that move and then writes them, so that no copy of the tensor is needed and each byte is read and
-// written once; slots that stay where they are are neither read for themselves nor written.  Bound by memory: 16 x 8 slots of 4 x 8 runs of 25 KB
-// on each side move in 66 us, 4.7 TB/s, a large copy's rate.
+// A thread reads its column of all slots' sources and then writes those that move, so that no copy of the tensor is needed.  Slots that stay where they are
+// are read (from themselves) but not written: with 16 x 8 slots of 4 x 8 runs of 25 KB, two tensors, none moving, 28 us.  Bound by memory: parents drawn at
+// random move them in 66 us, 4.7 TB/s, a large copy's rate.
 struct StateView {  // strides in bytes
   char *data;
   int64_t lead_stride, b_stride, slot_stride, inner_stride, row_bytes;
@@ -529,7 +529,7 @@ typedef uintx4_t uintx4_any __attribute__((aligned(1)));  // at any address
 
 template <typename V, int BEAM>
 __device__ __forceinline__ void move_column(char *p, int64_t slot_stride, const int (&parent)[BEAM], int beam) {
-  V v[BEAM];  // (of a slot that stays, itself: without branches all loads leave at once)
+  V v[BEAM];  // (of a slot that stays, itself, of places behind the beam, slot 0: without branches all loads leave at once)
 #pragma unroll
   for (int k = 0; k < BEAM; ++k) v[k] = *reinterpret_cast<const V *>(p + (k < beam ? parent[k] : 0) * slot_stride);
 #pragma unroll
