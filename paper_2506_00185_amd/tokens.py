@@ -260,7 +260,8 @@ class KVCache:
     def _set(self, k, v, k_exp, v_exp):
         import torch
         _refuse(k.dim() == 4 and k.dtype in (torch.float16, torch.float8_e4m3fn), "k must be [n_pages, heads, page_size, dim], float8_e4m3fn or float16")
-        _sizes(k.shape[0], k.shape[1])
+        for size in k.shape:
+            _sizes(size)
         _refuse(k.is_cuda, "tensors must be on the GPU: there is no CPU fallback")
         self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
         self.n_pages, self.heads, self.page_size, self.dim = k.shape

@@ -254,6 +254,9 @@ def test_sizes_that_32_bits_do_not_hold_are_refused(lib):
     states = [(meta(2, 3, big), 0), (meta(2, 3, big, 2)[..., :1], 0), (meta(big, 2, 3, 4), 1)]
     calls = [lambda: select_tokens(meta(2, 3, big), meta(2, 3, dtype=f64)), lambda: select_tokens(meta(big, 3, 7), meta(big, 3, dtype=f64)),
              lambda: KVCache.from_tensors(meta(big, 1, 1, 16), meta(big, 1, 1, 16), meta(big, 1, 1), meta(big, 1, 1)),
+             lambda: KVCache.from_tensors(meta(1, 1, 2**32 + 16, 16), meta(1, 1, 2**32 + 16, 16), meta(1, 1, 2**32 + 16), meta(1, 1, 2**32 + 16)),
+             lambda: KVCache.from_tensors(meta(1, 1, 16, 2**32 + 16), meta(1, 1, 16, 2**32 + 16), meta(1, 1, 16), meta(1, 1, 16)),
+             lambda: KVCache.from_tensors(meta(1, big, 1, 16), meta(1, big, 1, 16), meta(1, big, 1), meta(1, big, 1)),
              lambda: c.write(meta(3, big, 2, 64), meta(3, big, 2, 64), table, start), lambda: c.read(table, start, big),
              lambda: c.write(rows, rows, meta(3, big, dtype=i32), start), lambda: c.write(meta(big, 1, 2, 64), meta(big, 1, 2, 64), meta(big, 8, dtype=i32), meta(big, dtype=i32)),
              lambda: c.attend(meta(3, big, 2, 64), table, start), lambda: c.attend(meta(3, 1, big - 1, 64), table, start),
