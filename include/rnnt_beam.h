@@ -379,7 +379,7 @@ int rnnt_reorder_states(const int32_t *parent, int32_t B, int32_t beam, const rn
 /*
  * A paged cache of one attention layer's keys and values, in the caller's arrays.  A row, the `dim` values of one token and key head, is kept
  * as y 2^s: s the smallest exponent with max |x| <= 448 2^s (RNNT_CACHE_E4M3, y in OCP e4m3) or max |x| < 2^15 2^s (RNNT_CACHE_F16, y in
- * float16), at least -126; y = x 2^-s rounded to the nearest, ties to even.  A row with a NaN or an infinity is kept as y = 0, exponent byte 255 and reads
+ * float16), at least -126, 0 for a row of zeros; y = x 2^-s rounded to the nearest, ties to even.  A row with a NaN or an infinity is kept as y = 0, exponent byte 255 and reads
  * as NaN.  Position p of sequence b lies in page table[b, p / page_size], place p % page_size.  Positions that are negative or
  * beyond the table, and those whose page is outside 0 .. n_pages - 1, are not there: not written, read as zeros, not attended.
  */

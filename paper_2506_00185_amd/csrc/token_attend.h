@@ -387,7 +387,7 @@ __global__ __launch_bounds__(256, (Attend<TT, FMT, DP, MT>::WAVES)) void k_atten
           const int t = (j >> 2) * 16 + 4 * g4 + (j & 3);
           if (l16 == 0 && !(held >> (16 * g4) & 0xffff) && fabsf(mt.v_exp[t]) < INFINITY) {
             mt.v_exp[t] = (float)kZeroRow;
-            mt.v_inv[t] = 0x1p45f;
+            mt.v_inv[t] = __uint_as_float((uint32_t)(127 - kZeroRow) << 23);
           }
         }
         wave_lds_order();
